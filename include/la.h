@@ -19,8 +19,8 @@
  *
  * Conventions for every entry point
  *   - All tensor pointers are DEVICE pointers on the device that was current at la_create,
- *     16-byte aligned, densely packed, innermost dimension last.  Exceptions are marked
- *     "host".  q, k, v, o and the window use the io type of the context (fp32 or bf16);
+ *     16-byte aligned, densely packed (an la_view says its strides), innermost dimension last.
+ *     Exceptions are marked "host".  q, k, v, o and the window use the io type of the context (fp32 or bf16);
  *     S, z and the convolution weights are always fp32.
  *   - Calls are asynchronous on `stream` (a cudaStream_t passed as void*; NULL is the
  *     default stream).  No entry point other than la_create / la_destroy allocates or frees
@@ -94,6 +94,16 @@ typedef struct {
 } la_state;
 
 typedef struct la_ctx la_ctx;
+
+/* A tensor whose rows lie apart, as a projection leaves its heads: element (b, h, t, i) of [B, H, T, d] is at
+ * p[b sb + h sh + t st + i]; the d values of a row are dense.  Strides count elements, are not negative and, in bytes,
+ * are multiples of 16 below 2^40; p is 16-byte aligned; the stride of an axis of one element is ignored.  Rows of an
+ * axis that is read may coincide over b or h (stride 0: a tensor broadcast over sequences or heads), rows of different
+ * tokens may not (st >= d).  Rows that are written do not overlap one another nor anything the call reads. */
+typedef struct {
+  void*   p;
+  int64_t sb, sh, st;
+} la_view;
 
 /* Library set-up.  la_create validates the configuration, allocates the device status word
  * on the current device and returns a context; la_destroy frees it.  Neither is
@@ -259,6 +269,78 @@ la_status la_accept_greedy(la_ctx* ctx, int32_t B, int32_t N, const int32_t* par
  * status LA_ERR_BAD_TREE; LA_ERR_INVALID_ARG for null pointers or N outside 1..max_nodes. */
 la_status la_accept_threshold(la_ctx* ctx, int32_t B, int32_t N, const int32_t* parent, const float* score,
                               const float* thresh, int32_t* accept_node, int32_t* accept_len, void* stream);
+
+/* ---- Linear attention with a decay for each head ------------------------------------------------------------------
+ * (No counterpart in the paper, whose layer forgets nothing.)  lam_h = exp(log_decay[h]); no feature map, no normaliser,
+ * no convolution (of the context only H, d and the io type count):
+ *   S_i = lam_h S_{i-1} + k_i v_i^T,    o_i = scale q_i^T S_i
+ *       = scale (sum_{j<=i} lam_h^(i-j) (q_i . k_j) v_j + lam_h^(i+1) q_i^T S_in)
+ *
+ *   q, k, v, o   views [B, H, T, d], io type
+ *   log_decay    [H] fp32 device, at most 0 (0: nothing is forgotten; -inf: only the token itself is seen)
+ *   scale        finite; 1 / sqrt(d) is the usual choice
+ *   S_in, S_out  [B, H, d, d] fp32, S[a][c] with c (the value's index) innermost; S_in NULL: an empty state; S_out NULL:
+ *                not wanted.  They may be the same buffer.
+ *   lens         [B] int32 device or NULL (all T): the tokens of each sequence of a batch padded to T, 0 .. T.  What lies
+ *                in the rows behind a sequence's length is not used, whatever it is; the outputs' rows there are set to 0;
+ *                a sequence of length 0 leaves S_out = S_in.
+ *   pos          [B] int64 device or NULL: advanced by the tokens absorbed
+ *
+ * A head whose log_decay is above 0 or NaN, and a sequence whose length is outside 0 .. T, record LA_ERR_INVALID_ARG in
+ * the device status and are skipped: their outputs and states are left unwritten, and so is such a sequence's pos.
+ * A value of v that is not finite shows in its channel of the tokens from its own on; with the tensor-core kernels
+ * also in earlier tokens of its tile of 128.  The same holds for the gradients, in the direction in which they depend. */
+la_status la_decay_prefill(la_ctx* ctx, int32_t B, int32_t T, const la_view* q /*host struct*/, const la_view* k,
+                           const la_view* v, const float* log_decay, float scale, const float* S_in, float* S_out,
+                           const int32_t* lens, int64_t* pos, const la_view* o, void* stream);
+
+/* Gradients of la_decay_prefill: from do_ = dL/do and (where S_out is used) dS_out = dL/dS_out,
+ *   D_{len-1} = dS_out + scale q do^T of the last token,  D_{i-1} = lam D_i + scale q_{i-1} do_{i-1}^T,
+ *   dq_i = scale S_i do_i,   dk_i = D_i v_i,   dv_i = D_i^T k_i,   dS_in = lam D_0.
+ *   do_, dq, dk, dv  views [B, H, T, d], io type;  S_in, lens as in the forward call (S_in as it was before it)
+ *   dS_out           [B, H, d, d] fp32 or NULL (0);  dS_in [B, H, d, d] fp32 out, or NULL: not wanted; another buffer
+ * The gradients' rows behind a sequence's length are set to 0.  log_decay is a constant of the model and gets no
+ * gradient.  Heads that share a k or v (stride 0) get a gradient each; the caller adds them up. */
+la_status la_decay_backward(la_ctx* ctx, int32_t B, int32_t T, const la_view* q, const la_view* k, const la_view* v,
+                            const la_view* do_, const float* log_decay, float scale, const float* S_in,
+                            const float* dS_out, const int32_t* lens, const la_view* dq, const la_view* dk,
+                            const la_view* dv, float* dS_in, void* stream);
+
+/* One token per sequence: S = lam S + k v^T in place, o = scale q^T S.
+ *   q, k, v, o  views [B, H, 1, d] (st is ignored);  S [B, H, d, d] fp32 in-out;  pos [B] int64 or NULL: advanced by 1 */
+la_status la_decay_step(la_ctx* ctx, int32_t B, const la_view* q, const la_view* k, const la_view* v,
+                        const float* log_decay, float scale, float* S, int64_t* pos, const la_view* o, void* stream);
+
+/* Norms of the queries and keys of each head and the rotation by their positions, in one pass: what a layer without a
+ * feature map does to q and k.  Each row x of d values at position p = pos[b] + t becomes
+ *   y = x rsqrt(mean(x^2) + eps) w                      (norm = 0: y = x)
+ *   (y_a, y_b) <- mscale (y_a cos - y_b sin, y_b cos + y_a sin),  angle p inv_freq[m],  m < rot / 2
+ * with the pairs (a, b) = (m, m + rot / 2), or (2 m, 2 m + 1) if interleaved; values from rot on stay y.
+ * Angles are formed in 64 bits (positions may be far out), everything else in fp32. */
+typedef struct {
+  const float*   wq;            /* [d] fp32 device, weights of the norm; NULL: ones */
+  const float*   wk;
+  float          eps;           /* >= 0 */
+  int32_t        norm;          /* 0: rotation only (wq, wk and eps are not used) */
+  const double*  inv_freq;      /* [rot / 2] fp64 device; NULL if rot is 0 */
+  int32_t        rot;           /* values of a row that are rotated: a multiple of 16, 0 .. d */
+  int32_t        interleaved;
+  float          mscale;        /* factor of the rotated values (1; some long-context scalings use another) */
+  const int64_t* pos;           /* [B] int64 device: position of the first token of each sequence; NULL: 0 */
+} la_norm_rope_args;
+
+/* q, k -> qo, ko, views [B, H, T, d] of the io type; an output may be the input's own view (in place). */
+la_status la_norm_rope(la_ctx* ctx, int32_t B, int32_t T, const la_norm_rope_args* args /*host struct*/, const la_view* q,
+                       const la_view* k, const la_view* qo, const la_view* ko, void* stream);
+
+/* Its gradients: q and k as they went in, gq = dL/dqo, gk = dL/dko -> dq, dk (each may be the view gq, gk itself) and, over all rows,
+ * dwq, dwk [d] fp32 (both NULL: not wanted; they are overwritten; with norm = 0 they have to be NULL).
+ *   scratch  la_norm_rope_scratch_bytes(ctx) bytes of device memory where dwq, dwk are wanted (partial sums, added up in
+ *            a fixed order); else NULL.  Calls that may overlap need one each. */
+la_status la_norm_rope_backward(la_ctx* ctx, int32_t B, int32_t T, const la_norm_rope_args* args, const la_view* q,
+                                const la_view* k, const la_view* gq, const la_view* gk, const la_view* dq,
+                                const la_view* dk, float* dwq, float* dwk, float* scratch, void* stream);
+uint64_t  la_norm_rope_scratch_bytes(const la_ctx* ctx);
 
 /* Self-test of the bounded waits.  (No counterpart in the paper.)  Every wait of a kernel of this library on a
  * shared-memory barrier has a time limit, after which the kernel records LA_ERR_TIMEOUT in the status word and

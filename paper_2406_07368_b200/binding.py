@@ -36,7 +36,9 @@ EXPORTS = ["la_create", "la_destroy", "la_status_str", "la_prefill", "la_decode_
            "la_commit", "la_last_device_status", "la_clear_device_status", "la_set_prefill_kernel",
            "la_launch_count", "la_verify_tree_noalloc", "la_set_workspace", "la_accept_greedy", "la_selftest_wait_timeout",
            "la_prefill_workspace_bytes", "la_prefill_grouped", "la_prefill_grouped_max_group",
-           "la_segment_state", "la_state_prefix", "la_accept_threshold"]
+           "la_segment_state", "la_state_prefix", "la_accept_threshold",
+           "la_decay_prefill", "la_decay_backward", "la_decay_step", "la_norm_rope", "la_norm_rope_backward",
+           "la_norm_rope_scratch_bytes"]
 
 
 class LaError(RuntimeError):
@@ -49,6 +51,15 @@ class la_config(C.Structure):
     _fields_ = [("H", C.c_int32), ("d", C.c_int32), ("conv_taps", C.c_int32), ("chunk", C.c_int32),
                 ("phi", C.c_int), ("eps", C.c_float), ("io_dtype", C.c_int), ("max_nodes", C.c_int32),
                 ("max_depth", C.c_int32)]
+
+
+class la_view(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("sb", C.c_int64), ("sh", C.c_int64), ("st", C.c_int64)]
+
+
+class la_norm_rope_args(C.Structure):
+    _fields_ = [("wq", C.c_void_p), ("wk", C.c_void_p), ("eps", C.c_float), ("norm", C.c_int32), ("inv_freq", C.c_void_p),
+                ("rot", C.c_int32), ("interleaved", C.c_int32), ("mscale", C.c_float), ("pos", C.c_void_p)]
 
 
 class la_state(C.Structure):
@@ -83,6 +94,14 @@ def lib() -> C.CDLL:
         L.la_selftest_wait_timeout.argtypes = [vp, C.c_uint32, vp, vp]
         L.la_verify_tree_noalloc.argtypes = [C.POINTER(la_config), i32, i32, vp, vp, vp, vp, vp, C.POINTER(la_state),
                                              vp, vp, vp]
+        view, args, f32 = C.POINTER(la_view), C.POINTER(la_norm_rope_args), C.c_float
+        L.la_decay_prefill.argtypes = [vp, i32, i32, view, view, view, vp, f32, vp, vp, vp, vp, view, vp]
+        L.la_decay_backward.argtypes = [vp, i32, i32, view, view, view, view, vp, f32, vp, vp, vp, view, view, view, vp, vp]
+        L.la_decay_step.argtypes = [vp, i32, view, view, view, vp, f32, vp, vp, view, vp]
+        L.la_norm_rope.argtypes = [vp, i32, i32, args, view, view, view, view, vp]
+        L.la_norm_rope_backward.argtypes = [vp, i32, i32, args, view, view, view, view, view, view, vp, vp, vp, vp]
+        L.la_norm_rope_scratch_bytes.argtypes = [vp]
+        L.la_norm_rope_scratch_bytes.restype = C.c_uint64
         L.la_last_device_status.argtypes = [vp, vp]
         L.la_clear_device_status.argtypes = [vp, vp]
         L.la_set_prefill_kernel.argtypes = [vp, i32]
@@ -92,7 +111,8 @@ def lib() -> C.CDLL:
         L.la_prefill_workspace_bytes.restype = C.c_uint64
         L.la_launch_count.restype = C.c_int64
         for name in EXPORTS:
-            if name not in ("la_status_str", "la_launch_count", "la_prefill_workspace_bytes", "la_prefill_grouped_max_group"):
+            if name not in ("la_status_str", "la_launch_count", "la_prefill_workspace_bytes", "la_prefill_grouped_max_group",
+                            "la_norm_rope_scratch_bytes"):
                 getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -168,7 +188,7 @@ class Context:
         with torch.cuda.device(self.device):
             torch.cuda.current_stream()          # make sure the device context exists
             _check("la_create", lib().la_create(C.byref(cfg), C.byref(self._h)))
-        self._plan = _host_module().Plan(self._h.value, H, d, conv_taps, max_depth, io == "bf16")
+        self._plan = _host_module().Plan(self._h.value, H, d, conv_taps, max_depth, io == "bf16", self.device.index)
 
     def close(self) -> None:
         if self._h:
@@ -241,6 +261,33 @@ class Context:
 
     def la_accept_threshold(self, parent, score, thresh, accept_node=None, accept_len=None, stream=None):
         return self._plan.accept_threshold(parent, score, thresh, accept_node, accept_len, stream)
+
+    # The layer with a decay (see include/la.h).  q, k, v and the gradients may have any strides with dense rows; an output
+    # the caller does not bring has its axes in the order of q's.
+    def la_decay_prefill(self, q, k, v, log_decay, scale: float, S_in=None, S_out=None, lens=None, pos=None, out=None,
+                         stream=None):
+        return self._plan.decay_prefill(q, k, v, log_decay, scale, S_in, S_out, lens, pos, out, stream)
+
+    def la_decay_backward(self, q, k, v, do, log_decay, scale: float, S_in=None, dS_out=None, dS_in=None, lens=None,
+                          dq=None, dk=None, dv=None, stream=None):
+        """(dq, dk, dv); dS_in, where given, receives the gradient of S_in."""
+        return self._plan.decay_backward(q, k, v, do, log_decay, scale, S_in, dS_out, dS_in, lens, dq, dk, dv, stream)
+
+    def la_decay_step(self, q, k, v, log_decay, scale: float, S, pos=None, out=None, stream=None):
+        return self._plan.decay_step(q, k, v, log_decay, scale, S, pos, out, stream)
+
+    def la_norm_rope(self, q, k, wq, wk, eps: float, inv_freq, interleaved: bool = False, mscale: float = 1.0,
+                     norm: bool = True, pos=None, q_out=None, k_out=None, stream=None):
+        """(q, k) normalised and rotated; inv_freq [rot / 2] float64 (None: no rotation), see rope.inv_freq."""
+        return self._plan.norm_rope(q, k, wq, wk, eps, inv_freq, interleaved, mscale, norm, pos, q_out, k_out, stream)
+
+    def la_norm_rope_backward(self, q, k, gq, gk, wq, wk, eps: float, inv_freq, interleaved: bool = False,
+                              mscale: float = 1.0, norm: bool = True, pos=None, dq=None, dk=None, dwq=None, dwk=None,
+                              weights: bool = True, stream=None):
+        """(dq, dk, dwq, dwk) from gq, gk, the gradients of la_norm_rope's outputs; dwq, dwk None where norm or weights
+        is false."""
+        return self._plan.norm_rope_backward(q, k, gq, gk, wq, wk, eps, inv_freq, interleaved, mscale, norm, pos, dq, dk,
+                                             dwq, dwk, weights, stream)
 
     def la_selftest_wait_timeout(self, limit_us: int, stream=None) -> int:
         """Runs the bounded-wait self-test; returns the nanoseconds the wait took (see include/la.h)."""

@@ -1,0 +1,59 @@
+// Shared by the kernels of the layer with a decay.
+#pragma once
+#include "la_common.cuh"
+
+namespace la {
+
+// Length of sequence b: T without lens, -1 where the given length is outside 0 ... T.
+__device__ __forceinline__ int seq_len(const int32_t* lens, int b, int T) {
+  if (!lens) return T;
+  const int L = lens[b];
+  return L < 0 || L > T ? -1 : L;
+}
+__device__ __forceinline__ bool decay_ok(float g) { return g <= 0.f; }   // (a NaN is not)
+// lam^n, n >= 0; lam^0 = 1 for lam = 0 too.
+__device__ __forceinline__ float decay_pow(float g, int n) { return n == 0 ? 1.f : expf(g * (float)n); }
+// The same in two parts, for a state that fades slowly: rounded to fp32 the factor is off by up to 2^-25 in the same
+// direction at every step, which over the 1 / |g n| steps that such a state remembers adds up to 2^-25 / |g n|.  With what the
+// rounding left off (1 - hi is exact there) the error per step is |g n| 2^-24, and the sum stays at 2^-24.  A factor
+// below a half is forgotten too soon for that.  (hi x is the product that goes unrounded into the sum: lo x is less than
+// half a unit in its last place and would be lost behind a rounding.)
+struct Fade {
+  float hi, lo;
+  __device__ __forceinline__ float operator()(float x) const { return fmaf(hi, x, lo * x); }
+};
+__device__ __forceinline__ Fade decay_fade(float g, int n) {
+  const float x = n == 0 ? 0.f : g * (float)n, hi = expf(x);
+  return {hi, hi > 0.5f ? expm1f(x) + (1.f - hi) : 0.f};
+}
+
+template <typename T> struct Io8;   // eight consecutive values of the io type
+template <> struct Io8<float> {
+  static __device__ __forceinline__ void load(const float* p, float (&x)[8]) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  }
+  static __device__ __forceinline__ void store(float* p, const float (&x)[8]) {
+    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+  }
+};
+template <> struct Io8<__nv_bfloat16> {
+  static __device__ __forceinline__ void load(const __nv_bfloat16* p, float (&x)[8]) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+  static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&x)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
+}  // namespace la

@@ -1,0 +1,90 @@
+// One token of the layer with a decay: S = lam S + k v^T, o = scale q^T S.
+// The state is streamed through registers once, 128-bit loads all in flight before the first use, as in the decode step
+// of the layer without a decay.  The columns of S do not meet: where (sequence, head) units are too few to fill the GPU a
+// unit is cut into blocks of 32 columns, one thread block each, and nothing has to be added up across thread blocks.
+#include "decay.cuh"
+
+namespace la {
+namespace ds {
+
+constexpr int kThreads = 256;
+
+template <typename T, int D, int CB>
+__global__ void __launch_bounds__(kThreads)
+decay_step_kernel(const la_view q, const la_view k, const la_view v, const float* __restrict__ log_decay, float scale,
+                  float* __restrict__ S, int64_t* __restrict__ pos, const la_view o, int* status, int H) {
+  constexpr int TPR = CB / 4, RPP = kThreads / TPR, PASSES = D / RPP;
+  __shared__ __align__(16) float fq[D], fk[D], fv[CB];
+  __shared__ __align__(16) float red[RPP][CB];
+  const int bh = blockIdx.x, b = bh / H, h = bh % H, c0 = blockIdx.y * CB, t = threadIdx.x;
+  const int c4 = t % TPR * 4, rg = t / TPR;
+  float* Sb = S + (size_t)bh * D * D + c0;
+  pdl_wait();
+  pdl_trigger();
+  float4 s[PASSES];
+#pragma unroll
+  for (int m = 0; m < PASSES; ++m) s[m] = __ldcs(reinterpret_cast<const float4*>(Sb + (size_t)(rg + RPP * m) * D + c4));
+  const float g = log_decay[h];
+  if (t < D) {
+    fq[t] = to_f32(((const T*)q.p)[b * q.sb + h * q.sh + t]) * scale;
+    fk[t] = to_f32(((const T*)k.p)[b * k.sb + h * k.sh + t]);
+  } else if (t - D < CB) {
+    fv[t - D] = to_f32(((const T*)v.p)[b * v.sb + h * v.sh + c0 + t - D]);
+  }
+  if (pos && h == 0 && c0 == 0 && t == 0) pos[b] += 1;
+  if (!decay_ok(g)) {
+    if (t == 0) report(status, LA_ERR_INVALID_ARG);
+    return;
+  }
+  const Fade fade = decay_fade(g, 1);
+  __syncthreads();
+  const float4 v4 = *reinterpret_cast<const float4*>(&fv[c4]);
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int m = 0; m < PASSES; ++m) {
+    const int r = rg + RPP * m;
+    const float a = fk[r], x = fq[r];
+    s[m].x = fmaf(a, v4.x, fade(s[m].x));
+    s[m].y = fmaf(a, v4.y, fade(s[m].y));
+    s[m].z = fmaf(a, v4.z, fade(s[m].z));
+    s[m].w = fmaf(a, v4.w, fade(s[m].w));
+    acc.x = fmaf(x, s[m].x, acc.x);
+    acc.y = fmaf(x, s[m].y, acc.y);
+    acc.z = fmaf(x, s[m].z, acc.z);
+    acc.w = fmaf(x, s[m].w, acc.w);
+    __stcs(reinterpret_cast<float4*>(Sb + (size_t)r * D + c4), s[m]);
+  }
+  *reinterpret_cast<float4*>(&red[rg][c4]) = acc;
+  __syncthreads();
+  if (t < CB) {
+    float n = 0.f;
+#pragma unroll
+    for (int i = 0; i < RPP; ++i) n += red[i][t];
+    ((T*)o.p)[b * o.sb + h * o.sh + c0 + t] = from_f32<T>(n);
+  }
+}
+
+}  // namespace ds
+
+template <typename T, int D>
+static cudaError_t launch_step_t(la_ctx* ctx, int B, const la_view& q, const la_view& k, const la_view& v, const float* g,
+                                 float scale, float* S, int64_t* pos, const la_view& o, cudaStream_t s) {
+  const int units = B * ctx->cfg.H;
+  ctx->launches += 1;
+  if (units <= 2 * ctx->sm_count)
+    return launch_pdl(ds::decay_step_kernel<T, D, 32>, dim3(units, D / 32), dim3(ds::kThreads), 0, s, q, k, v, g, scale, S,
+                      pos, o, ctx->d_status, ctx->cfg.H);
+  return launch_pdl(ds::decay_step_kernel<T, D, D>, dim3(units, 1), dim3(ds::kThreads), 0, s, q, k, v, g, scale, S, pos, o,
+                    ctx->d_status, ctx->cfg.H);
+}
+
+cudaError_t launch_decay_step(la_ctx* ctx, int B, const la_view& q, const la_view& k, const la_view& v, const float* g,
+                              float scale, float* S, int64_t* pos, const la_view& o, cudaStream_t s) {
+  if (ctx->cfg.io_dtype == LA_F32)
+    return ctx->cfg.d == 64 ? launch_step_t<float, 64>(ctx, B, q, k, v, g, scale, S, pos, o, s)
+                            : launch_step_t<float, 128>(ctx, B, q, k, v, g, scale, S, pos, o, s);
+  return ctx->cfg.d == 64 ? launch_step_t<__nv_bfloat16, 64>(ctx, B, q, k, v, g, scale, S, pos, o, s)
+                          : launch_step_t<__nv_bfloat16, 128>(ctx, B, q, k, v, g, scale, S, pos, o, s);
+}
+
+}  // namespace la

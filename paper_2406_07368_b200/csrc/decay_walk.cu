@@ -1,0 +1,113 @@
+// The recurrence with a decay, token by token, in fp32 on the CUDA cores:
+//   X_n = lam X_{n-1} + upd k_n v_n^T,   o_n = r q_n^T X_n.
+// The columns of X do not meet, so a thread block takes 32 of them: warp w holds rows w D/8 ... of X in registers, one
+// column per lane, D/8 values per thread.  16 tokens at a time are staged in shared memory; inside a chunk the warps do
+// not wait for one another, and their parts of q_n^T X_n are added up behind it.
+#include "decay.cuh"
+
+namespace la {
+namespace dw {
+
+constexpr int kThreads = 256, kCols = 32, kStage = 16;
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads)
+decay_walk_kernel(const DecayPasses ps, const float* __restrict__ log_decay, const int32_t* __restrict__ lens,
+                  int64_t* __restrict__ pos, int* status, int H, int Tlen) {
+  constexpr int ROWS = D / 8;
+  __shared__ __align__(16) float sq[kStage][D], sk[kStage][D], sv[kStage][kCols];
+  __shared__ float part[kStage][8][kCols];
+  const DecayPass& p = ps.p[blockIdx.z];
+  const int bh = blockIdx.x, b = bh / H, h = bh % H, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int c0 = blockIdx.y * kCols;
+  pdl_wait();
+  pdl_trigger();
+  const float g = log_decay[h];
+  const int L = seq_len(lens, b, Tlen);
+  if (pos && L > 0 && h == 0 && blockIdx.y == 0 && blockIdx.z == 0 && tid == 0) pos[b] += L;
+  if (L < 0 || !decay_ok(g)) {
+    if (tid == 0) report(status, LA_ERR_INVALID_ARG);
+    return;
+  }
+  const T* q = (const T*)p.q.p + b * p.q.sb + h * p.q.sh;
+  const T* k = (const T*)p.k.p + b * p.k.sb + h * p.k.sh;
+  const T* v = (const T*)p.v.p + b * p.v.sb + h * p.v.sh + c0;
+  T* o = (T*)p.o.p + b * p.o.sb + h * p.o.sh + c0;
+  const size_t sbase = (size_t)bh * D * D;
+  const int a0 = warp * ROWS;
+  float x[ROWS];
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i)
+    x[i] = p.S_in ? p.S_in[sbase + (p.trans ? (size_t)(c0 + lane) * D + a0 + i : (size_t)(a0 + i) * D + c0 + lane)] : 0.f;
+  const Fade fade = decay_fade(g, 1);
+
+  for (int n0 = 0; n0 < L; n0 += kStage) {
+    const int nt = min(kStage, L - n0);
+    auto row = [&](int j) { return (int64_t)(p.rev ? L - 1 - (n0 + j) : n0 + j); };
+    __syncthreads();                                         // (the chunk before has been read)
+    for (int i = tid; i < nt * (D / 8); i += kThreads) {
+      const int j = i / (D / 8), e = i % (D / 8) * 8;
+      float y[8];
+      Io8<T>::load(q + row(j) * p.q.st + e, y);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) sq[j][e + t] = y[t] * p.r;
+      Io8<T>::load(k + row(j) * p.k.st + e, y);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) sk[j][e + t] = y[t] * p.upd;
+    }
+    for (int i = tid; i < nt * kCols; i += kThreads) sv[i / kCols][i % kCols] = to_f32(v[row(i / kCols) * p.v.st + i % kCols]);
+    __syncthreads();
+    for (int j = 0; j < nt; ++j) {
+      const float vv = sv[j][lane];
+      const Fade f = p.rev && n0 + j == 0 ? Fade{1.f, 0.f} : fade;
+      float acc = 0.f;
+#pragma unroll
+      for (int i = 0; i < ROWS; i += 4) {
+        const float4 kk = *reinterpret_cast<const float4*>(&sk[j][a0 + i]);
+        const float4 qq = *reinterpret_cast<const float4*>(&sq[j][a0 + i]);
+        const float ka[4] = {kk.x, kk.y, kk.z, kk.w}, qa[4] = {qq.x, qq.y, qq.z, qq.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[i + e] = fmaf(ka[e], vv, f(x[i + e]));
+          acc = fmaf(qa[e], x[i + e], acc);
+        }
+      }
+      part[j][warp][lane] = acc;
+    }
+    __syncthreads();
+    for (int i = tid; i < nt * kCols; i += kThreads) {
+      const int j = i / kCols, c = i % kCols;
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) s += part[j][w][c];
+      o[row(j) * p.o.st + c] = from_f32<T>(s);
+    }
+  }
+  for (int64_t i = (int64_t)L * kCols + tid; i < (int64_t)Tlen * kCols; i += kThreads)
+    o[i / kCols * p.o.st + i % kCols] = from_f32<T>(0.f);    // rows behind the sequence
+  if (p.S_out) {
+    const Fade f = p.rev && L > 0 ? fade : Fade{1.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) p.S_out[sbase + (size_t)(a0 + i) * D + c0 + lane] = f(x[i]);
+  }
+}
+
+}  // namespace dw
+
+template <typename T>
+static cudaError_t launch_walk_t(la_ctx* ctx, int B, int T_, const DecayPasses& ps, const float* g, const int32_t* lens,
+                                 int64_t* pos, cudaStream_t s) {
+  const la_config& c = ctx->cfg;
+  ctx->launches += 1;
+  auto kern = c.d == 64 ? dw::decay_walk_kernel<T, 64> : dw::decay_walk_kernel<T, 128>;
+  return launch_pdl(kern, dim3(B * c.H, c.d / dw::kCols, ps.n), dim3(dw::kThreads), 0, s, ps, g, lens, pos, ctx->d_status,
+                    c.H, T_);
+}
+
+cudaError_t launch_decay_walk(la_ctx* ctx, int B, int T, const DecayPasses& ps, const float* log_decay, const int32_t* lens,
+                              int64_t* pos, cudaStream_t s) {
+  return ctx->cfg.io_dtype == LA_F32 ? launch_walk_t<float>(ctx, B, T, ps, log_decay, lens, pos, s)
+                                     : launch_walk_t<__nv_bfloat16>(ctx, B, T, ps, log_decay, lens, pos, s);
+}
+
+}  // namespace la

@@ -8,6 +8,7 @@
 
 #include <ATen/EmptyTensor.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -25,6 +26,7 @@ struct Plan {
   la_ctx* ctx;
   int64_t H, d, W, max_depth;
   at::ScalarType io;
+  int device;
 };
 
 PyObject *s_S, *s_z, *s_win, *s_pos, *s_cuda_stream, *g_error;   // interned names; the binding's exception class
@@ -52,7 +54,8 @@ const at::Tensor& tensor(PyObject* o, const char* name) {
   return THPVariable_Unpack(o);
 }
 const char* dtype_name(at::ScalarType t) {
-  return t == at::kFloat ? "torch.float32" : t == at::kBFloat16 ? "torch.bfloat16" : t == at::kInt ? "torch.int32" : "torch.int64";
+  return t == at::kFloat ? "torch.float32" : t == at::kBFloat16 ? "torch.bfloat16" : t == at::kInt ? "torch.int32"
+         : t == at::kDouble ? "torch.float64" : "torch.int64";
 }
 using Shape = std::initializer_list<int64_t>;
 
@@ -380,11 +383,235 @@ PyObject* accept_threshold(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- the layer with a decay ----
+// Its calls run on the context's device whatever the current one is: every tensor has to be there, and the stream, where
+// the caller names none, is that device's current one.
+void on_device(const Plan* p, const at::Tensor& t, const char* name) {
+  if (t.is_cuda() && t.device().index() == p->device) return;
+  PyErr_Format(PyExc_ValueError, "%s must be a CUDA tensor on device %d", name, p->device);
+  throw Raised();
+}
+void* dense(const Plan* p, PyObject* o, at::ScalarType dtype, Shape shape, const char* name) {
+  if (o != Py_None) on_device(p, tensor(o, name), name);
+  return ptr(o, dtype, shape, name);
+}
+void* stream_on(const Plan* p, PyObject* o) {
+  return o == Py_None ? (void*)c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)p->device).stream() : stream_of(o);
+}
+// A [B, H, T, d] tensor (step: [B, H, d]) of the io type with dense rows and any strides; null for None.
+la_view view(const Plan* p, PyObject* o, Shape shape, const char* name) {
+  if (o == Py_None) return {nullptr, 0, 0, 0};
+  const at::Tensor& t = tensor(o, name);
+  on_device(p, t, name);
+  if (t.scalar_type() != p->io) {
+    PyErr_Format(PyExc_ValueError, "%s must have dtype %s", name, dtype_name(p->io));
+    throw Raised();
+  }
+  if (t.sizes() != at::IntArrayRef(shape)) {
+    PyObject* want = PyTuple_New((Py_ssize_t)shape.size());
+    if (!want) throw Raised();
+    Py_ssize_t i = 0;
+    for (int64_t x : shape) PyTuple_SET_ITEM(want, i++, PyLong_FromLongLong(x));
+    PyErr_Format(PyExc_ValueError, "%s must have shape %R", name, want);
+    Py_DECREF(want);
+    throw Raised();
+  }
+  if (t.stride(-1) != 1) {
+    PyErr_Format(PyExc_ValueError, "%s must have dense rows (a last stride of 1)", name);
+    throw Raised();
+  }
+  return {t.data_ptr(), t.stride(0), t.stride(1), t.dim() == 4 ? t.stride(2) : p->d};
+}
+// The given tensor, or a new one whose axes lie in the order of `like` (heads of a token side by side, or tokens of a head).
+struct ViewOut {
+  PyObject* obj = nullptr;
+  la_view v;
+  ViewOut(const Plan* p, PyObject* given, const at::Tensor& like, Shape shape, const char* name) {
+    if (given != Py_None) {
+      v = view(p, given, shape, name);
+      Py_INCREF(given);
+      obj = given;
+      return;
+    }
+    const bool by_token = like.dim() == 4 && like.size(1) > 1 && like.size(2) > 1 && like.stride(1) < like.stride(2);
+    at::Tensor t;
+    if (by_token) {
+      const int64_t Hn = like.size(1), Tn = like.size(2), d = like.size(3);
+      t = at::detail::empty_strided_cuda(at::IntArrayRef(shape), {Tn * Hn * d, d, Hn * d, 1}, p->io, like.device());
+    } else {
+      t = at::detail::empty_cuda(at::IntArrayRef(shape), p->io, like.device(), std::nullopt);
+    }
+    v = {t.data_ptr(), t.stride(0), t.stride(1), t.dim() == 4 ? t.stride(2) : p->d};
+    obj = THPVariable_Wrap(std::move(t));
+    if (!obj) throw Raised();
+  }
+  ViewOut(const ViewOut&) = delete;
+  ~ViewOut() { Py_XDECREF(obj); }
+  PyObject* release() {
+    PyObject* o = obj;
+    obj = nullptr;
+    return o;
+  }
+};
+// Sizes go to the library as 32-bit numbers.
+int32_t size32(int64_t n, const char* what) {
+  if (n > INT32_MAX) {
+    PyErr_Format(PyExc_ValueError, "%s is too large", what);
+    throw Raised();
+  }
+  return (int32_t)n;
+}
+PyObject* tuple_of(std::initializer_list<PyObject*> items) {   // takes the references
+  PyObject* t = PyTuple_New((Py_ssize_t)items.size());
+  Py_ssize_t i = 0;
+  for (PyObject* o : items) {
+    if (t) PyTuple_SET_ITEM(t, i++, o);
+    else Py_DECREF(o);
+  }
+  if (!t) throw Raised();
+  return t;
+}
+
+// (q, k, v, log_decay, scale, S_in, S_out, lens, pos, out, stream)
+PyObject* decay_prefill(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Plan* p = (Plan*)self;
+  return method(n, 11, [&] {
+    const at::Tensor& q = lead(a[0], 4, "q");
+    const int64_t B = q.size(0), T = q.size(2);
+    const Shape shp = {B, p->H, T, p->d}, sshp = {B, p->H, p->d, p->d};
+    const la_view qv = view(p, a[0], shp, "q"), kv = view(p, a[1], shp, "k"), vv = view(p, a[2], shp, "v");
+    const float* g = (const float*)dense(p, a[3], at::kFloat, {p->H}, "log_decay");
+    const float scale = real(a[4]);
+    const float* S_in = (const float*)dense(p, a[5], at::kFloat, sshp, "S_in");
+    float* S_out = (float*)dense(p, a[6], at::kFloat, sshp, "S_out");
+    const int32_t* lens = (const int32_t*)dense(p, a[7], at::kInt, {B}, "lens");
+    int64_t* pos = (int64_t*)dense(p, a[8], at::kLong, {B}, "pos");
+    const int32_t B32 = size32(B, "the batch"), T32 = size32(T, "the length");
+    ViewOut o(p, a[9], q, shp, "out");
+    void* s = stream_on(p, a[10]);
+    check("la_decay_prefill", unlocked([&] { return la_decay_prefill(p->ctx, B32, T32, &qv, &kv, &vv, g, scale, S_in, S_out, lens, pos, &o.v, s); }));
+    return o.release();
+  });
+}
+// (q, k, v, do, log_decay, scale, S_in, dS_out, dS_in, lens, dq, dk, dv, stream)
+PyObject* decay_backward(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Plan* p = (Plan*)self;
+  return method(n, 14, [&] {
+    const at::Tensor& q = lead(a[0], 4, "q");
+    const int64_t B = q.size(0), T = q.size(2);
+    const Shape shp = {B, p->H, T, p->d}, sshp = {B, p->H, p->d, p->d};
+    const la_view qv = view(p, a[0], shp, "q"), kv = view(p, a[1], shp, "k"), vv = view(p, a[2], shp, "v"),
+                  dov = view(p, a[3], shp, "do");
+    const float* g = (const float*)dense(p, a[4], at::kFloat, {p->H}, "log_decay");
+    const float scale = real(a[5]);
+    const float* S_in = (const float*)dense(p, a[6], at::kFloat, sshp, "S_in");
+    const float* dS_out = (const float*)dense(p, a[7], at::kFloat, sshp, "dS_out");
+    float* dS_in = (float*)dense(p, a[8], at::kFloat, sshp, "dS_in");
+    const int32_t* lens = (const int32_t*)dense(p, a[9], at::kInt, {B}, "lens");
+    const int32_t B32 = size32(B, "the batch"), T32 = size32(T, "the length");
+    ViewOut dq(p, a[10], q, shp, "dq"), dk(p, a[11], q, shp, "dk"), dv(p, a[12], q, shp, "dv");
+    void* s = stream_on(p, a[13]);
+    check("la_decay_backward", unlocked([&] {
+            return la_decay_backward(p->ctx, B32, T32, &qv, &kv, &vv, &dov, g, scale, S_in, dS_out, lens, &dq.v, &dk.v, &dv.v,
+                                     dS_in, s);
+          }));
+    return tuple_of({dq.release(), dk.release(), dv.release()});
+  });
+}
+// (q, k, v, log_decay, scale, S, pos, out, stream)
+PyObject* decay_step(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Plan* p = (Plan*)self;
+  return method(n, 9, [&] {
+    const at::Tensor& q = lead(a[0], 3, "q");
+    const int64_t B = q.size(0);
+    const Shape shp = {B, p->H, p->d};
+    const la_view qv = view(p, a[0], shp, "q"), kv = view(p, a[1], shp, "k"), vv = view(p, a[2], shp, "v");
+    const float* g = (const float*)dense(p, a[3], at::kFloat, {p->H}, "log_decay");
+    const float scale = real(a[4]);
+    float* S = (float*)dense(p, a[5], at::kFloat, {B, p->H, p->d, p->d}, "S");
+    int64_t* pos = (int64_t*)dense(p, a[6], at::kLong, {B}, "pos");
+    const int32_t B32 = size32(B, "the batch");
+    ViewOut o(p, a[7], q, shp, "out");
+    void* s = stream_on(p, a[8]);
+    check("la_decay_step", unlocked([&] { return la_decay_step(p->ctx, B32, &qv, &kv, &vv, g, scale, S, pos, &o.v, s); }));
+    return o.release();
+  });
+}
+// (wq, wk, eps, inv_freq, interleaved, mscale, norm, pos) at a[0 ...]
+la_norm_rope_args rope_args(const Plan* p, PyObject* const* a, int64_t B) {
+  la_norm_rope_args r = {};
+  r.wq = (const float*)dense(p, a[0], at::kFloat, {p->d}, "wq");
+  r.wk = (const float*)dense(p, a[1], at::kFloat, {p->d}, "wk");
+  r.eps = real(a[2]);
+  if (a[3] != Py_None) {
+    const at::Tensor& f = lead(a[3], 1, "inv_freq");
+    r.inv_freq = (const double*)dense(p, a[3], at::kDouble, {f.size(0)}, "inv_freq");
+    r.rot = size32(2 * f.size(0), "inv_freq");
+  }
+  r.interleaved = truth(a[4]);
+  r.mscale = real(a[5]);
+  r.norm = truth(a[6]);
+  r.pos = (const int64_t*)dense(p, a[7], at::kLong, {B}, "pos");
+  return r;
+}
+// (q, k, <args>, q_out, k_out, stream)
+PyObject* norm_rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Plan* p = (Plan*)self;
+  return method(n, 13, [&] {
+    const at::Tensor& q = lead(a[0], 4, "q");
+    const int64_t B = q.size(0), T = q.size(2);
+    const Shape shp = {B, p->H, T, p->d};
+    const la_view qv = view(p, a[0], shp, "q"), kv = view(p, a[1], shp, "k");
+    const la_norm_rope_args r = rope_args(p, a + 2, B);
+    const int32_t B32 = size32(B, "the batch"), T32 = size32(T, "the length");
+    ViewOut qo(p, a[10], q, shp, "q_out"), ko(p, a[11], q, shp, "k_out");
+    void* s = stream_on(p, a[12]);
+    check("la_norm_rope", unlocked([&] { return la_norm_rope(p->ctx, B32, T32, &r, &qv, &kv, &qo.v, &ko.v, s); }));
+    return tuple_of({qo.release(), ko.release()});
+  });
+}
+// (q, k, gq, gk, <args>, dq, dk, dwq, dwk, weights, stream); weights: whether the weights' gradients are wanted
+PyObject* norm_rope_backward(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Plan* p = (Plan*)self;
+  return method(n, 18, [&] {
+    const at::Tensor& q = lead(a[0], 4, "q");
+    const int64_t B = q.size(0), T = q.size(2);
+    const Shape shp = {B, p->H, T, p->d};
+    const la_view qv = view(p, a[0], shp, "q"), kv = view(p, a[1], shp, "k"), gq = view(p, a[2], shp, "gq"), gk = view(p, a[3], shp, "gk");
+    const la_norm_rope_args r = rope_args(p, a + 4, B);
+    const int32_t B32 = size32(B, "the batch"), T32 = size32(T, "the length");
+    ViewOut dq(p, a[12], q, shp, "dq"), dk(p, a[13], q, shp, "dk");
+    void* s = stream_on(p, a[17]);
+    if (!truth(a[16]) || !r.norm) {
+      check("la_norm_rope_backward", unlocked([&] {
+              return la_norm_rope_backward(p->ctx, B32, T32, &r, &qv, &kv, &gq, &gk, &dq.v, &dk.v, nullptr, nullptr, nullptr, s);
+            }));
+      Py_INCREF(Py_None);
+      Py_INCREF(Py_None);
+      return tuple_of({dq.release(), dk.release(), Py_None, Py_None});
+    }
+    if (a[14] != Py_None) on_device(p, tensor(a[14], "dwq"), "dwq");
+    if (a[15] != Py_None) on_device(p, tensor(a[15], "dwk"), "dwk");
+    Out dwq(a[14], q, at::kFloat, {p->d}, "dwq"), dwk(a[15], q, at::kFloat, {p->d}, "dwk");
+    // The partial sums: memory of this call's stream, given back to the allocator when the call is enqueued (whoever
+    // gets it next on that stream comes behind the kernels).
+    const c10::cuda::CUDAStream cur = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)p->device);
+    at::Tensor scratch = at::detail::empty_cuda({(int64_t)(la_norm_rope_scratch_bytes(p->ctx) / 4)}, at::kFloat, q.device(), std::nullopt);
+    if (s != (void*)cur.stream())
+      c10::cuda::CUDACachingAllocator::recordStream(scratch.storage().data_ptr(), c10::cuda::getStreamFromExternal((cudaStream_t)s, (c10::DeviceIndex)p->device));
+    float* sp = (float*)scratch.data_ptr();
+    check("la_norm_rope_backward", unlocked([&] {
+            return la_norm_rope_backward(p->ctx, B32, T32, &r, &qv, &kv, &gq, &gk, &dq.v, &dk.v, (float*)dwq.p, (float*)dwk.p, sp, s);
+          }));
+    return tuple_of({dq.release(), dk.release(), dwq.release(), dwk.release()});
+  });
+}
+
 PyObject* plan_new(PyTypeObject* type, PyObject* args, PyObject*) {
   unsigned long long handle;
   long long H, d, W, max_depth;
-  int bf16;
-  if (!PyArg_ParseTuple(args, "KLLLLp", &handle, &H, &d, &W, &max_depth, &bf16)) return nullptr;
+  int bf16, device;
+  if (!PyArg_ParseTuple(args, "KLLLLpi", &handle, &H, &d, &W, &max_depth, &bf16, &device)) return nullptr;
   Plan* p = (Plan*)type->tp_alloc(type, 0);
   if (!p) return nullptr;
   p->ctx = reinterpret_cast<la_ctx*>((uintptr_t)handle);
@@ -393,6 +620,7 @@ PyObject* plan_new(PyTypeObject* type, PyObject* args, PyObject*) {
   p->W = W;
   p->max_depth = max_depth;
   p->io = bf16 ? at::kBFloat16 : at::kFloat;
+  p->device = device;
   return (PyObject*)p;
 }
 void plan_dealloc(PyObject* self) { Py_TYPE(self)->tp_free(self); }
@@ -403,6 +631,8 @@ PyObject* plan_close(PyObject* self, PyObject*) {   // calls after this get LA_E
 #define LA_FAST(f) {#f, (PyCFunction)(void (*)(void)) f, METH_FASTCALL, nullptr}
 PyMethodDef plan_methods[] = {LA_FAST(prefill), LA_FAST(prefill_grouped), LA_FAST(decode_step), LA_FAST(verify_tree),
                               LA_FAST(commit), LA_FAST(accept_greedy), LA_FAST(accept_threshold),
+                              LA_FAST(decay_prefill), LA_FAST(decay_backward), LA_FAST(decay_step), LA_FAST(norm_rope),
+                              LA_FAST(norm_rope_backward),
                               {"close", plan_close, METH_NOARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyTypeObject PlanType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 

@@ -3,6 +3,7 @@
 #include <cmath>
 #include <cstdlib>
 #include <new>
+#include <utility>
 
 #include "la_common.cuh"
 #include "la_internal.h"
@@ -23,6 +24,32 @@ bool state_ok(const la_ctx* ctx, const la_state* st) {
   return true;
 }
 
+// A view the kernels can take: in place of the stride of an axis of one element stands a harmless one, so that nobody
+// below looks at it.  Written rows may not overlap: the axes, from the smallest stride up, each step over all before it.
+bool view_ok(const la_ctx* ctx, const la_view* in, int64_t B, int64_t T, bool written, la_view* out) {
+  if (!in || !good(in->p)) return false;
+  const int64_t H = ctx->cfg.H, d = ctx->cfg.d, es = ctx->cfg.io_dtype == LA_F32 ? 4 : 2;
+  *out = *in;
+  if (B == 1) out->sb = 0;
+  if (H == 1) out->sh = 0;
+  if (T == 1) out->st = d;
+  for (int64_t s : {out->sb, out->sh, out->st})
+    if (s < 0 || s % (16 / es) || s >= ((int64_t)1 << 40) / es) return false;
+  if (out->st < d) return false;
+  if (!written) return true;
+  int64_t stride[3] = {out->sb, out->sh, out->st}, size[3] = {B, H, T};
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2 - i; ++j)
+      if (stride[j] > stride[j + 1]) std::swap(stride[j], stride[j + 1]), std::swap(size[j], size[j + 1]);
+  int64_t span = d;
+  for (int i = 0; i < 3; ++i) {
+    if (size[i] == 1) continue;
+    if (stride[i] < span) return false;
+    span += stride[i] * (size[i] - 1);
+  }
+  return true;
+}
+
 struct DeviceGuard {
   int prev = -1;
   bool ok = true;
@@ -33,6 +60,20 @@ struct DeviceGuard {
   }
   ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
 };
+
+// An output at the address of an input is that input's own view.
+bool in_place_ok(const la_view& in, const la_view& out) {
+  return in.p != out.p || (in.sb == out.sb && in.sh == out.sh && in.st == out.st);
+}
+bool norm_rope_args_ok(const la_ctx* ctx, const la_norm_rope_args* a) {
+  if (!a || a->rot < 0 || a->rot > ctx->cfg.d || a->rot % 16 || (a->rot && !a->inv_freq) || !std::isfinite(a->mscale)) return false;
+  return !a->norm || (std::isfinite(a->eps) && a->eps >= 0.f && aligned16(a->wq) && aligned16(a->wk));
+}
+// The sweeps of one call of the layer with a decay.
+la_status decay_sweeps(la_ctx* ctx, int B, int T, const la::DecayPasses& ps, const float* log_decay, const int32_t* lens,
+                       int64_t* pos, cudaStream_t s) {
+  return cuda_status(la::launch_decay_walk(ctx, B, T, ps, log_decay, lens, pos, s));
+}
 
 }  // namespace
 
@@ -268,6 +309,102 @@ la_status la_accept_threshold(la_ctx* ctx, int32_t B, int32_t N, const int32_t* 
                                      static_cast<cudaStream_t>(stream)) == cudaSuccess
              ? LA_OK
              : LA_ERR_CUDA;
+}
+
+la_status la_decay_prefill(la_ctx* ctx, int32_t B, int32_t T, const la_view* q, const la_view* k, const la_view* v,
+                           const float* log_decay, float scale, const float* S_in, float* S_out, const int32_t* lens,
+                           int64_t* pos, const la_view* o, void* stream) {
+  if (!ctx || B < 1 || T < 1 || !log_decay || !std::isfinite(scale) || !aligned16(S_in) || !aligned16(S_out))
+    return LA_ERR_INVALID_ARG;
+  la::DecayPasses ps = {};
+  la::DecayPass& p = ps.p[0];
+  if (!view_ok(ctx, q, B, T, false, &p.q) || !view_ok(ctx, k, B, T, false, &p.k) || !view_ok(ctx, v, B, T, false, &p.v) ||
+      !view_ok(ctx, o, B, T, true, &p.o) || o->p == q->p || o->p == k->p || o->p == v->p)
+    return LA_ERR_INVALID_ARG;
+  if ((int64_t)B * ctx->cfg.H > INT32_MAX) return LA_ERR_TOO_LARGE;
+  ps.n = 1;
+  p.S_in = S_in;
+  p.S_out = S_out;
+  p.r = scale;
+  p.upd = 1.f;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return LA_ERR_CUDA;
+  return decay_sweeps(ctx, B, T, ps, log_decay, lens, pos, static_cast<cudaStream_t>(stream));
+}
+
+la_status la_decay_backward(la_ctx* ctx, int32_t B, int32_t T, const la_view* q, const la_view* k, const la_view* v,
+                            const la_view* do_, const float* log_decay, float scale, const float* S_in, const float* dS_out,
+                            const int32_t* lens, const la_view* dq, const la_view* dk, const la_view* dv, float* dS_in,
+                            void* stream) {
+  if (!ctx || B < 1 || T < 1 || !log_decay || !std::isfinite(scale) || !aligned16(S_in) || !aligned16(dS_out) ||
+      !aligned16(dS_in) || (dS_in && (dS_in == S_in || dS_in == dS_out)))
+    return LA_ERR_INVALID_ARG;
+  la_view in[4], out[3];
+  const la_view *given[4] = {q, k, v, do_}, *wanted[3] = {dq, dk, dv};
+  for (int i = 0; i < 4; ++i)
+    if (!view_ok(ctx, given[i], B, T, false, &in[i])) return LA_ERR_INVALID_ARG;
+  for (int i = 0; i < 3; ++i) {
+    if (!view_ok(ctx, wanted[i], B, T, true, &out[i])) return LA_ERR_INVALID_ARG;
+    for (const la_view& x : in)
+      if (out[i].p == x.p) return LA_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (out[i].p == out[j].p) return LA_ERR_INVALID_ARG;
+  }
+  if ((int64_t)B * ctx->cfg.H > INT32_MAX) return LA_ERR_TOO_LARGE;
+  la::DecayPasses ps = {};
+  ps.n = 3;
+  ps.p[0] = {in[3], in[2], in[1], out[0], S_in, nullptr, scale, 1.f, 0, 1};
+  ps.p[1] = {in[2], in[3], in[0], out[1], dS_out, nullptr, 1.f, scale, 1, 1};
+  ps.p[2] = {in[1], in[0], in[3], out[2], dS_out, dS_in, 1.f, scale, 1, 0};
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return LA_ERR_CUDA;
+  return decay_sweeps(ctx, B, T, ps, log_decay, lens, nullptr, static_cast<cudaStream_t>(stream));
+}
+
+la_status la_decay_step(la_ctx* ctx, int32_t B, const la_view* q, const la_view* k, const la_view* v,
+                        const float* log_decay, float scale, float* S, int64_t* pos, const la_view* o, void* stream) {
+  if (!ctx || B < 1 || !log_decay || !std::isfinite(scale) || !good(S)) return LA_ERR_INVALID_ARG;
+  la_view vq, vk, vv, vo;
+  if (!view_ok(ctx, q, B, 1, false, &vq) || !view_ok(ctx, k, B, 1, false, &vk) || !view_ok(ctx, v, B, 1, false, &vv) ||
+      !view_ok(ctx, o, B, 1, true, &vo) || o->p == q->p || o->p == k->p || o->p == v->p)
+    return LA_ERR_INVALID_ARG;
+  if ((int64_t)B * ctx->cfg.H > INT32_MAX) return LA_ERR_TOO_LARGE;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return LA_ERR_CUDA;
+  return cuda_status(la::launch_decay_step(ctx, B, vq, vk, vv, log_decay, scale, S, pos, vo, static_cast<cudaStream_t>(stream)));
+}
+
+uint64_t la_norm_rope_scratch_bytes(const la_ctx* ctx) { return ctx ? la::norm_rope_scratch_bytes(ctx) : 0; }
+
+la_status la_norm_rope(la_ctx* ctx, int32_t B, int32_t T, const la_norm_rope_args* a, const la_view* q, const la_view* k,
+                       const la_view* qo, const la_view* ko, void* stream) {
+  if (!ctx || B < 1 || T < 1 || !norm_rope_args_ok(ctx, a)) return LA_ERR_INVALID_ARG;
+  la_view vq, vk, oq, ok;
+  if (!view_ok(ctx, q, B, T, false, &vq) || !view_ok(ctx, k, B, T, false, &vk) || !view_ok(ctx, qo, B, T, true, &oq) ||
+      !view_ok(ctx, ko, B, T, true, &ok) || !in_place_ok(vq, oq) || !in_place_ok(vk, ok) || oq.p == ok.p || oq.p == vk.p || ok.p == vq.p)
+    return LA_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return LA_ERR_CUDA;
+  return cuda_status(la::launch_norm_rope(ctx, B, T, *a, vq, vk, oq, ok, static_cast<cudaStream_t>(stream)));
+}
+
+la_status la_norm_rope_backward(la_ctx* ctx, int32_t B, int32_t T, const la_norm_rope_args* a, const la_view* q,
+                                const la_view* k, const la_view* gq, const la_view* gk, const la_view* dq,
+                                const la_view* dk, float* dwq, float* dwk, float* scratch, void* stream) {
+  if (!ctx || B < 1 || T < 1 || !norm_rope_args_ok(ctx, a) || (dwq == nullptr) != (dwk == nullptr) ||
+      (dwq && (!a->norm || !good(scratch) || dwq == dwk)))
+    return LA_ERR_INVALID_ARG;
+  la_view vq, vk, gvq, gvk, oq, ok;
+  if (!view_ok(ctx, q, B, T, false, &vq) || !view_ok(ctx, k, B, T, false, &vk) || !view_ok(ctx, gq, B, T, false, &gvq) ||
+      !view_ok(ctx, gk, B, T, false, &gvk) || !view_ok(ctx, dq, B, T, true, &oq) || !view_ok(ctx, dk, B, T, true, &ok))
+    return LA_ERR_INVALID_ARG;
+  if (!in_place_ok(gvq, oq) || !in_place_ok(gvk, ok) || oq.p == ok.p || oq.p == vq.p || oq.p == vk.p || oq.p == gvk.p ||
+      ok.p == vq.p || ok.p == vk.p || ok.p == gvq.p)
+    return LA_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return LA_ERR_CUDA;
+  return cuda_status(la::launch_norm_rope_backward(ctx, B, T, *a, vq, vk, gvq, gvk, oq, ok, dwq, dwk, scratch,
+                                                   static_cast<cudaStream_t>(stream)));
 }
 
 la_status la_last_device_status(la_ctx* ctx, void* stream) {

@@ -186,6 +186,33 @@ cudaError_t launch_segment_state_tc(la_ctx* ctx, int B, int T, const void* k, co
                                     cudaStream_t s, bool* handled);
 cudaError_t launch_state_prefix(la_ctx* ctx, const float* parts, const float* base, float* out, size_t n, int count,
                                 cudaStream_t s);
+// One sweep of the recurrence with a decay over B sequences of up to T tokens, forwards or backwards in time (rev), with
+// the roles of the tensors named as in the forward call:
+//   X_n = lam X_{n-1} + upd k_n v_n^T,   o_n = r q_n^T X_n,   n = 0 ... len - 1 counted in the direction of the sweep;
+// X_{-1} = S_in (transposed if trans); backwards, X_0 = S_in + upd k_0 v_0^T (S_in is then the gradient of the state
+// behind the last token).  S_out = X_{len-1}; backwards lam X_{len-1}.  The forward call is one sweep; a backward pass
+// is three: dq = (do, v, k) forwards from S_in^T, dk = (v, do, q) and dv = (k, q, do) backwards.
+struct DecayPass {
+  la_view q, k, v, o;
+  const float* S_in;
+  float* S_out;
+  float r, upd;
+  int rev, trans;
+};
+struct DecayPasses {
+  DecayPass p[3];
+  int n;
+};
+cudaError_t launch_decay_walk(la_ctx* ctx, int B, int T, const DecayPasses& ps, const float* log_decay, const int32_t* lens,
+                              int64_t* pos, cudaStream_t s);
+cudaError_t launch_decay_step(la_ctx* ctx, int B, const la_view& q, const la_view& k, const la_view& v,
+                              const float* log_decay, float scale, float* S, int64_t* pos, const la_view& o, cudaStream_t s);
+cudaError_t launch_norm_rope(la_ctx* ctx, int B, int T, const la_norm_rope_args& a, const la_view& q, const la_view& k,
+                             const la_view& qo, const la_view& ko, cudaStream_t s);
+cudaError_t launch_norm_rope_backward(la_ctx* ctx, int B, int T, const la_norm_rope_args& a, const la_view& q,
+                                      const la_view& k, const la_view& gq, const la_view& gk, const la_view& dq,
+                                      const la_view& dk, float* dwq, float* dwk, float* scratch, cudaStream_t s);
+size_t norm_rope_scratch_bytes(const la_ctx* ctx);
 // Workspace la_prefill can use for a launch of B sequences of T tokens (0: none needed).
 size_t prefill_workspace_bytes(const la_ctx* ctx, int B, int T);
 }  // namespace la
