@@ -1,0 +1,758 @@
+// The recurrence with a decay on the 5th-generation tensor cores (bf16 io), chunkwise: tiles of 128 tokens, for prefill
+// and, run forwards and backwards in time with the roles of the tensors exchanged, for its gradients (DecayPass).
+//
+// In a tile of n tokens, X the state before it, a token's age counted in the direction of the sweep:
+//   o_i = r upd sum_{j no later than i} lam^(i-j) (q_i . k_j) v_j  +  r lam^(i+1) q_i^T X
+//   X  <- lam^n X + upd sum_j lam^(n-1-j) k_j v_j^T
+// Four products per tile run as tcgen05.mma with their accumulators in TMEM:
+//   P  = Q K^T            O1 = (P o M) V          M_ij = r upd lam^(i-j), 0 above the diagonal; P o M as bf16 back to TMEM
+//   O2 = Q X              X as bf16 in shared memory; the factor r lam^(i+1) belongs to a row, i.e. to a thread of the
+//                         epilogue, which adds o = O1 + r lam^(i+1) O2
+//   dX = K~^T V           K~_j = upd lam^(n-1-j) k_j, as two bf16 numbers (hi + lo) per value
+// The state is fp32, and a user is handed it: k rounded to bf16 behind its factor would leave it 2^-9 off per term; hi + lo
+// is 2^-17 off and costs one more product, which the tensor cores have time for.  X itself stays in the registers of
+// 256 threads (X = lam^n X + dX), so that no tile waits for another one's accumulator.
+//
+// Roles, side by side: warps 0-3 mask P, warps 4-7 write the outputs, warps 8-15 hold X and make K~ and the bf16 copy of X,
+// one lane of warp 16 issues the products, one of warp 17 the TMA loads into a ring of tiles.
+// No factor is formed as lam^i lam^-j, which overflows for heads that forget fast: 32 columns at a time share the exponent
+// of their nearest one, which is never negative, and the diagonal blocks take theirs from a table.
+// Few chains of a long sequence: a cluster of up to 16 blocks takes one chain, a segment each.  Every block first forms
+// the sum of its own segment (K and V are then read twice), leaves it in its shared memory, adds up those before it
+// through distributed shared memory, and all segments run at once.  No workspace, one launch.
+// What bounds it: HBM where chains fill the GPU.  Every wait is bounded; see la_common.cuh.
+#include <cuda.h>
+
+#include "decay.cuh"
+
+namespace la {
+namespace dtc {
+
+constexpr int TILE = 128;
+constexpr int kThreadsA = 128, kThreadsB = 128, kThreadsC = 256, kMmaWarp = 16 /* its fellows 17 (loads), 18, 19 */, kThreads = 640;
+// Registers per thread once the roles have traded theirs: the launch gives everyone 96, per scheduler five warps of them.
+constexpr int kRegsA = 72, kRegsB = 88, kRegsC = 128, kRegsIssue = 64;
+static_assert(kRegsA + kRegsB + 2 * kRegsC + kRegsIssue == 5 * 96, "register split");
+constexpr uint32_t BOX = 128 * 128;                // 128 rows x 64 bf16, 128-byte swizzle
+constexpr uint32_t SC_COL = 0, O1_COL = 128, O2_COL = 256, DX_COL = 384, TMEM_COLS = 512;
+constexpr int kMaxSeg = 16;
+
+template <int D> struct Map {
+  static constexpr uint32_t SLOT = D / 64 * BOX;   // a tile of q, k or v
+  static constexpr int NSLOT = D == 128 ? 5 : 9;
+  // lo behind the ring; X as bf16: 128 rows (d = 64: rows 0-63 the part of X from hi, 64-127 that from lo)
+  static constexpr uint32_t OFF_LO = NSLOT * SLOT, OFF_X = OFF_LO + SLOT, OFF_CTL = OFF_X + SLOT;
+};
+struct Ctl {
+  unsigned long long bars[40];
+  float tab[64];                                   // 32 + x: r upd lam^|x| where column x of a diagonal block, counted from
+                                                   // the row's own, is not later than the row, else 0
+  float col[32];                                   // lam to the distance between column j and the nearest of its 32 columns
+  uint32_t tmem_base;
+  int abort;
+};
+// KRDY and LO exist twice: the state pass makes K~ of a tile while the product of the one before runs.  Every other barrier
+// completes once per tile, and nobody completes it again before its waiters have passed.
+enum { B_FULL = 0, B_EMPTY = 10, B_QKD = 20, B_PRDY, B_KRDY0, B_KRDY1, B_DXD, B_XRDY, B_OD, B_OF, B_SHARED, B_TAKEN, B_DRAIN,
+       kNumBars };
+static_assert(kNumBars <= 40, "Ctl::bars");
+template <int D> constexpr uint32_t smem_bytes() { return Map<D>::OFF_CTL + (uint32_t)sizeof(Ctl) + 1024u; }
+static_assert(smem_bytes<128>() <= 227u * 1024u && smem_bytes<64>() <= 227u * 1024u, "shared memory");
+static_assert(smem_bytes<64>() > 114u * 1024u, "one block per SM: each allocates all of the TMEM");
+
+// mbar_wait with one answer for the whole warp: what follows a wait is done by all of its lanes or by none.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort));
+}
+
+// ---- PTX ----
+template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(n) : "memory"); }
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ uint32_t map_rank(uint32_t addr, int rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void mbar_arrive_remote(uint32_t bar, int rank) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_rank(bar, rank)) : "memory");
+}
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort) {
+  const uint32_t t0 = global_ns();
+  do {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    if (ok) return true;
+  } while (!*abort && global_ns() - t0 <= kWaitLimitNs);
+  *abort = 1;
+  return false;
+}
+__device__ __forceinline__ float4 ld_cluster(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ void sync_c() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int t, int h, int b, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      ::"r"(dst), "l"(map), "r"(x), "r"(t), "r"(h), "r"(b), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+      : "memory");
+}
+// A from TMEM; blocks of 32 rows of the accumulator whose mask is all ones are left as they are.
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool acc, uint32_t m0, uint32_t m1,
+                                       uint32_t m2, uint32_t m3) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %6, %7, %8}, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc),
+      "r"((uint32_t)acc), "r"(m0), "r"(m1), "r"(m2), "r"(m3)
+      : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Shared-memory matrix descriptors (128-byte swizzle, 8-row groups 1024 bytes apart), low words; the steps of a product
+// differ in the start address only, by a constant.  (Formed anew for every instruction they cost the issuing lane more
+// than the tensor cores take for it.)  The address is masked: in a cluster its upper bits say whose shared memory it is.
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lbo) { return ((addr >> 4) & 0x3FFFu) | ((lbo >> 4) << 16); }
+__device__ __forceinline__ uint64_t desc(uint32_t lo) {
+  return ((uint64_t)((1024u >> 4) | (1u << 14) | (2u << 29)) << 32) | lo;
+}
+// Step ks of 16 values where the contraction index runs along the 128-byte rows, ...
+__host__ __device__ constexpr uint32_t step_k(int ks) { return ((uint32_t)(ks >> 2) * BOX + (uint32_t)(ks & 3) * 32u) >> 4; }
+// ... or of 16 rows where it runs along the rows of the tile (the leading offset then leads to the next 64 columns).
+__host__ __device__ constexpr uint32_t step_mn(int ks) { return (uint32_t)ks * 2048u >> 4; }
+// bf16 x bf16 with fp32 sums, M = 128, N = n; a_mn, b_mn: that operand's contraction index runs along the rows of its tile.
+__host__ __device__ constexpr uint32_t idesc(bool a_mn, bool b_mn, uint32_t n) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
+// 16-byte piece 0 of row `row` of a swizzled box; piece i is at this address (of a box that starts on 128 bytes) ^ 16 i.
+__device__ __forceinline__ uint32_t row_at(int row) { return (uint32_t)row * 128u + (uint32_t)((row & 7) << 4); }
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float lo_f(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float hi_f(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+// (volatile: read where they are used, tile after tile, instead of kept in 32 registers)
+__device__ __forceinline__ float lds(uint32_t a) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ float4 lds4(uint32_t a) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+// The same value, but what is computed from it is computed here, not ahead of the loop and kept in registers.
+__device__ __forceinline__ uint32_t here(uint32_t x) {
+  asm volatile("" : "+r"(x));
+  return x;
+}
+__device__ __forceinline__ float asf(uint32_t u) { return __uint_as_float(u); }
+
+// A place in the ring of tiles, and the parity of the loads that land there.
+template <int N> struct Ring {
+  uint32_t s = 0, phase = 0;
+  __device__ __forceinline__ Ring next() const { return s + 1 == N ? Ring{0u, phase ^ 1u} : Ring{s + 1, phase}; }
+};
+struct Sweep {
+  la_view o;
+  const float* S_in;
+  float* S_out;
+  float r, upd;
+  int rev, trans;
+  int mq, mk, mv;                                  // which tensor maps
+};
+struct alignas(64) Args {
+  CUtensorMap map[4];
+  int hmul[4], bmul[4];                            // 0: the tensor is broadcast over heads / sequences
+  Sweep sw[3];
+  int n;
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log_decay, const int32_t* __restrict__ lens,
+                int64_t* __restrict__ pos, int* status, int H, int Tlen, int nseg, int early) {
+  using M = Map<D>;
+  constexpr uint32_t SLOT = M::SLOT;
+  constexpr int NSLOT = M::NSLOT, NX = D / 2;      // NX: values of X per thread of group C
+  extern __shared__ unsigned char smem_dyn[];
+  unsigned char* smem = smem_dyn + ((1024u - (smem_u32(smem_dyn) & 1023u)) & 1023u);
+  const uint32_t sbase = smem_u32(smem);
+  Ctl& ctl = *reinterpret_cast<Ctl*>(smem + M::OFF_CTL);
+  volatile int* abort = &ctl.abort;
+  const uint32_t bars = smem_u32(&ctl.bars[0]);
+  auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = (int)blockIdx.x % nseg, chain = (int)blockIdx.x / nseg;
+  const int bh = chain / args.n, b = bh / H, h = bh % H;
+  const Sweep& sw = args.sw[chain % args.n];
+
+  // ---- set-up: barriers, TMEM ----
+  if (tid == 0) {
+    for (int i = 0; i < NSLOT; ++i) {
+      mbar_init(bar(B_FULL + i), 1);
+      mbar_init(bar(B_EMPTY + i), 1);
+    }
+    mbar_init(bar(B_QKD), 1);
+    mbar_init(bar(B_PRDY), kThreadsA);
+    mbar_init(bar(B_KRDY0), kThreadsC);
+    mbar_init(bar(B_KRDY1), kThreadsC);
+    mbar_init(bar(B_DXD), 1);
+    mbar_init(bar(B_XRDY), kThreadsC);
+    mbar_init(bar(B_OD), 1);
+    mbar_init(bar(B_OF), kThreadsB);
+    mbar_init(bar(B_SHARED), rank > 0 ? rank : 1);                 // from every block before this one
+    mbar_init(bar(B_TAKEN), rank < nseg - 1 ? nseg - 1 - rank : 1);  // from every block behind it
+    mbar_init(bar(B_DRAIN), 1);
+    ctl.abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl.tmem_base)), "r"(TMEM_COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  pdl_wait();
+  if (early) pdl_trigger();
+  const float g = log_decay[h];
+  const int L = seq_len(lens, b, Tlen);
+  const bool bad = L < 0 || !decay_ok(g);
+  if (tid >= 64 && tid < 96) ctl.col[lane] = bad ? 0.f : decay_pow(g, sw.rev ? lane : 31 - lane);
+  if (tid < 64) {
+    const int x = sw.rev ? tid - 32 : 32 - tid;
+    ctl.tab[tid] = x < 0 || bad ? 0.f : sw.r * sw.upd * decay_pow(g, x);
+  }
+  tc_before();
+  __syncthreads();
+  tc_after();
+  if (nseg > 1) cluster_sync();                    // the others' barriers exist before anybody arrives on them
+  const uint32_t tmem = ctl.tmem_base;
+  if (pos && L > 0 && chain % args.n == 0 && rank == 0 && h == 0 && tid == 0) pos[b] += L;
+  if (bad && tid == 0) report(status, LA_ERR_INVALID_ARG);
+
+  // Tokens n0 ... n1 - 1 of the sweep are this block's, in whole tiles but for the sequence's last one.
+  const int rev = sw.rev;
+  const int tiles_all = bad ? 0 : (L + TILE - 1) / TILE, seg = (tiles_all + nseg - 1) / nseg * TILE;
+  const int n0 = min(L, rank * seg), n1 = min(L, n0 + seg);
+  const int nt = bad ? 0 : (n1 - n0 + TILE - 1) / TILE;
+  const int ns = nseg > 1 && rank < nseg - 1 ? nt : 0;             // tiles of the state pass
+  auto count = [&](int t) { return min(TILE, n1 - n0 - t * TILE); };   // tokens of tile t
+  auto first = [&](int t) {                        // token in row 0 (backwards: may be negative, those rows read as zeros)
+    const int s = n0 + t * TILE;
+    return rev ? L - s - TILE : s;
+  };
+
+  if (warp < 4) {
+    // =============================== group A: P -> P o M ===============================
+    regs_down<kRegsA>();
+    float base[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) base[i] = bad ? 0.f : sw.r * sw.upd * decay_pow(g, rev ? 32 * (i + 1) - lane : 32 * (i + 1) - 31 + lane);
+    const uint32_t diag = smem_u32(ctl.tab + 32) - 4u * (uint32_t)lane, col = smem_u32(ctl.col);
+    const uint32_t seen_cols = rev ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);   // of the diagonal block
+    const uint32_t t0 = tmem + SC_COL + ((uint32_t)(warp * 32) << 16);
+    for (int t = 0; t < nt; ++t) {
+      if (!warp_wait(bar(B_QKD), t & 1, abort)) break;
+      tc_after();
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {                // 32 columns; this warp's rows meet them all, in part or not at all
+        const int ahead = rev ? c - warp : warp - c;
+        uint32_t p[16];
+        if (ahead < 0) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) p[j] = 0u;
+        } else {
+          uint32_t s[32];
+          tmem_ld32(t0 + 32u * c, s);
+          tmem_wait_ld();
+          if (ahead == 0) {
+            const uint32_t m = here(seen_cols);
+            // (a select: behind the diagonal a score that is not finite must not meet the factor 0)
+#pragma unroll
+            for (int j = 0; j < 32; j += 2)
+              p[j / 2] = pack2(m >> j & 1u ? asf(s[j]) * lds(diag + 4u * j) : 0.f, m >> (j + 1) & 1u ? asf(s[j + 1]) * lds(diag + 4u * (j + 1)) : 0.f);
+          } else {
+            const float f = ahead == 1 ? base[0] : ahead == 2 ? base[1] : base[2];
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+              const float4 w = lds4(col + 4u * j);
+              p[j / 2] = pack2(asf(s[j]) * (f * w.x), asf(s[j + 1]) * (f * w.y));
+              p[j / 2 + 1] = pack2(asf(s[j + 2]) * (f * w.z), asf(s[j + 3]) * (f * w.w));
+            }
+          }
+        }
+        tmem_st16(t0 + 16u * c, p);                // over columns of its own rows that have been read
+      }
+      tmem_wait_st();
+      tc_before();
+      mbar_arrive(bar(B_PRDY));
+    }
+  } else if (warp < 8) {
+    // =============================== group B: outputs ===============================
+    regs_down<kRegsB>();
+    const int row = (warp - 4) * 32 + lane, age = rev ? TILE - 1 - row : row;
+    const uint32_t tl = tmem + ((uint32_t)((warp - 4) * 32) << 16);
+    __nv_bfloat16* o = (__nv_bfloat16*)sw.o.p + b * sw.o.sb + h * sw.o.sh;
+    const float f_all = bad ? 0.f : sw.r * decay_pow(g, age + 1), f_first = bad ? 0.f : sw.r * decay_pow(g, age);
+    for (int t = 0; t < nt; ++t) {
+      if (!warp_wait(bar(B_OD), t & 1, abort)) break;
+      tc_after();
+      const float f = rev && n0 + t == 0 ? f_first : f_all;        // (a sweep backwards starts from the gradient as it is)
+      const bool live = age < count(t);
+      __nv_bfloat16* to = o + (int64_t)(first(t) + row) * sw.o.st;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) {
+        uint32_t x[16], y[16];
+        tmem_ld16(tl + O1_COL + 16u * c, x);
+        tmem_ld16(tl + O2_COL + 16u * c, y);
+        tmem_wait_ld();
+        if (c == D / 16 - 1) {
+          tc_before();
+          mbar_arrive(bar(B_OF));
+        }
+        if (live) {
+          uint32_t w[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) w[i] = pack2(fmaf(f, asf(y[2 * i]), asf(x[2 * i])), fmaf(f, asf(y[2 * i + 1]), asf(x[2 * i + 1])));
+          *reinterpret_cast<uint4*>(to + 16 * c) = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(to + 16 * c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+      }
+    }
+    if (!bad)                                      // rows behind the sequence
+      for (int64_t i = (int64_t)L * (D / 8) + rank * kThreadsB + (tid - 128); i < (int64_t)Tlen * (D / 8); i += (int64_t)nseg * kThreadsB)
+        *reinterpret_cast<uint4*>(o + i / (D / 8) * sw.o.st + i % (D / 8) * 8) = make_uint4(0u, 0u, 0u, 0u);
+  } else if (warp < 16) {
+    // =============================== group C: X, K~, X as bf16 ===============================
+    regs_up<kRegsC>();
+    const int ct = tid - 256, q4 = warp & 3, hf = (warp - 8) >> 2, a = 32 * q4 + lane;   // row a of X, columns hf NX ...
+    const int krow = ct & 127, kage = rev ? TILE - 1 - krow : krow, kh = ct >> 7;        // a row and a half of a tile
+    const uint32_t tx = tmem + DX_COL + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(hf * NX);
+    const bool real = D == 128 || q4 < 2;          // d = 64: rows 64 ... hold the part of X that comes from lo
+    const size_t sat = ((size_t)bh * D + a) * D + hf * NX;
+    // (d = 64: the second half of a row starts at its piece 4)
+    const uint32_t k_at = D == 128 ? (uint32_t)kh * BOX + row_at(krow) : row_at(krow) ^ (64u * kh);
+    const uint32_t x_at = D == 128 ? (uint32_t)hf * BOX + row_at(a) : row_at(a) ^ (64u * hf);
+    float X[NX];
+#pragma unroll
+    for (int i = 0; i < NX; ++i) X[i] = 0.f;
+    const float k_full = bad ? 0.f : sw.upd * decay_pow(g, TILE - 1 - kage);
+    const Fade fade_full = decay_fade(bad ? 0.f : g, TILE);
+    Ring<NSLOT> ring;
+    uint32_t made = 0, seen = 0;                   // tiles of K~ made, products dX waited for
+    bool ok = true;
+
+    // K~ of a tile: hi in the place of K, lo beside it.  Rows without a token are zeros in K~ and (they may hold anything
+    // where the sequence is shorter than the tensor) in V.
+    auto make_k = [&](Ring<NSLOT> rk, Ring<NSLOT> rv, int n, uint32_t lo_at) -> bool {
+      if (!warp_wait(bar(B_FULL + rk.s), rk.phase, abort)) return false;
+      const uint32_t at = sbase + here(k_at), kp = at + rk.s * SLOT, lp = at + lo_at;
+      const bool live = kage < n;
+      const float f = n == TILE ? k_full : live ? sw.upd * decay_pow(g, n - 1 - kage) : 0.f;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        const uint4 u = lds128(kp ^ (16u * i));
+        const uint32_t in[4] = {u.x, u.y, u.z, u.w};
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float x = lo_f(in[j]), y = hi_f(in[j]);
+          hi[j] = live ? pack2(x * f, y * f) : 0u;
+          lo[j] = live ? pack2(fmaf(x, f, -lo_f(hi[j])), fmaf(y, f, -hi_f(hi[j]))) : 0u;
+        }
+        sts128(kp ^ (16u * i), hi[0], hi[1], hi[2], hi[3]);
+        sts128(lp ^ (16u * i), lo[0], lo[1], lo[2], lo[3]);
+      }
+      if (n < TILE) {
+        if (!warp_wait(bar(B_FULL + rv.s), rv.phase, abort)) return false;
+        if (!live) {
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) sts128((at + rv.s * SLOT) ^ (16u * i), 0u, 0u, 0u, 0u);
+        }
+      }
+      fence_async();
+      mbar_arrive(bar(made & 1 ? B_KRDY1 : B_KRDY0));
+      ++made;
+      return true;
+    };
+    // X = lam^n X + dX
+    auto take_dx = [&](const Fade& f) -> bool {
+      if (!warp_wait(bar(B_DXD), seen & 1, abort)) return false;
+      ++seen;
+      tc_after();
+#pragma unroll
+      for (int c = 0; c < NX / 32; ++c) {
+        uint32_t x[32];
+        tmem_ld32(tx + 32u * c, x);
+        tmem_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) X[32 * c + j] = f(X[32 * c + j]) + asf(x[j]);
+      }
+      tc_before();
+      return true;
+    };
+    auto write_x = [&] {                           // the bf16 copy: rows of X are rows of the tile
+      const uint32_t xp = sbase + M::OFF_X + here(x_at);
+#pragma unroll
+      for (int i = 0; i < NX / 8; ++i)
+        sts128(xp ^ (16u * i), pack2(X[8 * i], X[8 * i + 1]), pack2(X[8 * i + 2], X[8 * i + 3]), pack2(X[8 * i + 4], X[8 * i + 5]),
+               pack2(X[8 * i + 6], X[8 * i + 7]));
+      fence_async();
+    };
+
+    if (nseg > 1) {                                // (a bad head's blocks pass through with zeros and write nothing)
+      // the sum of this block's segment, from nothing
+      if (ns > 0) ok = make_k(ring, ring.next(), count(0), M::OFF_LO);
+      for (int t = 0; ok && t < ns; ++t) {
+        ring = ring.next().next();
+        if (t + 1 < ns) ok = make_k(ring, ring.next(), count(t + 1), t & 1 ? M::OFF_LO : M::OFF_X);
+        if (!ok || !take_dx(count(t) == TILE ? fade_full : decay_fade(g, count(t)))) { ok = false; break; }
+        mbar_arrive(bar(B_XRDY));
+      }
+      if (rank < nseg - 1) {
+#pragma unroll
+        for (int i = 0; i < NX / 4; ++i)
+          *reinterpret_cast<float4*>(smem + M::OFF_LO + (uint32_t)(i * kThreadsC + ct) * 16u) =
+              make_float4(X[4 * i], X[4 * i + 1], X[4 * i + 2], X[4 * i + 3]);
+        sync_c();
+        if (ct == 0) {
+          asm volatile("fence.acq_rel.cluster;" ::: "memory");
+          for (int s = rank + 1; s < nseg; ++s) mbar_arrive_remote(bar(B_SHARED), s);
+        }
+      }
+    }
+    // X before the segment: the caller's state, then the sums of the segments before this one
+    if (sw.S_in && real && !bad) {
+      if (sw.trans) {
+        const float* p = sw.S_in + ((size_t)bh * D + hf * NX) * D + a;
+#pragma unroll
+        for (int i = 0; i < NX; ++i) X[i] = p[(size_t)i * D];
+      } else {
+#pragma unroll
+        for (int i = 0; i < NX; i += 4) {
+          const float4 v = *reinterpret_cast<const float4*>(sw.S_in + sat + i);
+          X[i] = v.x, X[i + 1] = v.y, X[i + 2] = v.z, X[i + 3] = v.w;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NX; ++i) X[i] = 0.f;
+    }
+    if (nseg > 1) {
+      if (rank > 0) {
+        ok = __all_sync(0xffffffffu, mbar_wait_cluster(bar(B_SHARED), 0, abort)) && ok;
+        for (int s = 0; ok && s < rank; ++s) {
+          const int ls = min(L, (s + 1) * seg) - min(L, s * seg);
+          const Fade f = decay_fade(bad ? 0.f : g, ls > 0 ? ls - (s == 0 ? rev : 0) : 0);
+          const uint32_t from = map_rank(sbase + M::OFF_LO, s);
+#pragma unroll
+          for (int i = 0; i < NX / 4; ++i) {
+            const float4 v = ld_cluster(from + (uint32_t)(i * kThreadsC + ct) * 16u);
+            X[4 * i] = f(X[4 * i]) + v.x;
+            X[4 * i + 1] = f(X[4 * i + 1]) + v.y;
+            X[4 * i + 2] = f(X[4 * i + 2]) + v.z;
+            X[4 * i + 3] = f(X[4 * i + 3]) + v.w;
+          }
+        }
+        sync_c();
+        if (ct == 0)
+          for (int s = 0; s < rank; ++s) mbar_arrive_remote(bar(B_TAKEN), s);
+      }
+      if (rank < nseg - 1) ok = __all_sync(0xffffffffu, mbar_wait_cluster(bar(B_TAKEN), 0, abort)) && ok;
+    }
+    if (ok && nt > 0) {
+      write_x();
+      mbar_arrive(bar(B_XRDY));
+    }
+    for (int t = 0; ok && t < nt; ++t) {
+      const int n = count(t), e = rev && n0 + t == 0;
+      ok = warp_wait(bar(B_QKD), t & 1, abort);    // K has been read as it is
+      if (!ok || !make_k(ring, ring.next().next(), n, M::OFF_LO)) { ok = false; break; }
+      ring = ring.next().next().next();
+      if (!take_dx(n == TILE && !e ? fade_full : decay_fade(g, n - e))) { ok = false; break; }
+      if (t + 1 < nt) {
+        write_x();
+        mbar_arrive(bar(B_XRDY));
+      }
+    }
+    if (sw.S_out && !bad && rank == nseg - 1) {    // (the barrier inside is for every thread, whatever its waits said)
+      const Fade f = decay_fade(g, rev && L > 0 ? 1 : 0);
+      if (D == 64) {                               // the two parts meet (lo is free: its last product has completed)
+        if (!real)
+#pragma unroll
+          for (int i = 0; i < NX / 4; ++i)
+            *reinterpret_cast<float4*>(smem + M::OFF_LO + (uint32_t)((i * 2 + hf) * 64 + a - 64) * 16u) =
+                make_float4(X[4 * i], X[4 * i + 1], X[4 * i + 2], X[4 * i + 3]);
+        sync_c();
+        if (real)
+#pragma unroll
+          for (int i = 0; i < NX / 4; ++i) {
+            const float4 v = *reinterpret_cast<const float4*>(smem + M::OFF_LO + (uint32_t)((i * 2 + hf) * 64 + a) * 16u);
+            X[4 * i] += v.x, X[4 * i + 1] += v.y, X[4 * i + 2] += v.z, X[4 * i + 3] += v.w;
+          }
+      }
+      if (real && ok)
+#pragma unroll
+        for (int i = 0; i < NX; i += 4)
+          *reinterpret_cast<float4*>(sw.S_out + sat + i) = make_float4(f(X[i]), f(X[i + 1]), f(X[i + 2]), f(X[i + 3]));
+    }
+  } else {
+    regs_down<kRegsIssue>();
+    if (tid == kMmaWarp * 32) {
+      // =============================== products ===============================
+      bool ok = true;
+      uint32_t made = 0, x_at = 0;
+      Ring<NSLOT> rk;
+      const uint32_t lo_at = sbase + M::OFF_LO;
+      auto landed = [&](const Ring<NSLOT>& r) { return mbar_wait(bar(B_FULL + r.s), r.phase, abort); };
+      auto k_made = [&] {
+        const uint32_t i = made++;
+        return mbar_wait(bar(B_KRDY0) + 8u * (i & 1), (i >> 1) & 1, abort);
+      };
+      auto dx = [&](uint32_t kt, uint32_t vt, uint32_t lo) {
+        const uint32_t v_lo = desc_lo(vt, BOX);
+        if (D == 128) {
+          const uint32_t hi_d = desc_lo(kt, BOX), lo_d = desc_lo(lo, BOX);
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks) mma(tmem + DX_COL, desc(hi_d + step_mn(ks)), desc(v_lo + step_mn(ks)), idesc(true, true, 128), ks > 0);
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks) mma(tmem + DX_COL, desc(lo_d + step_mn(ks)), desc(v_lo + step_mn(ks)), idesc(true, true, 128), true);
+        } else {                                   // hi and lo side by side: rows 0-63 and 64-127 of one product
+          const uint32_t k_d = desc_lo(kt, lo - kt);
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks) mma(tmem + DX_COL, desc(k_d + step_mn(ks)), desc(v_lo + step_mn(ks)), idesc(true, true, 64), ks > 0);
+        }
+        mma_commit(bar(B_DXD));
+      };
+      for (int t = 0; t < ns; ++t) {
+        const Ring<NSLOT> rv = rk.next();
+        ok = landed(rv) && k_made();
+        if (ok && t > 0) ok = mbar_wait(bar(B_XRDY), x_at++ & 1, abort);       // the sum before has been read
+        if (!ok) break;
+        tc_after();
+        dx(sbase + rk.s * SLOT, sbase + rv.s * SLOT, t & 1 ? sbase + M::OFF_X : lo_at);
+        mma_commit(bar(B_EMPTY + rk.s));
+        mma_commit(bar(B_EMPTY + rv.s));
+        rk = rv.next();
+      }
+      if (ok && ns > 0) ok = mbar_wait(bar(B_XRDY), x_at++ & 1, abort);
+      for (int t = 0; ok && t < nt; ++t) {
+        const Ring<NSLOT> rq = rk.next(), rv = rq.next();
+        const uint32_t x_lo = desc_lo(here(sbase) + M::OFF_X, BOX), q_lo = desc_lo(sbase + rq.s * SLOT, 16u), k_lo = desc_lo(sbase + rk.s * SLOT, 16u);
+        ok = landed(rk) && landed(rq);
+        if (!ok) break;
+        tc_after();
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) mma(tmem + SC_COL, desc(q_lo + step_k(ks)), desc(k_lo + step_k(ks)), idesc(false, false, 128), ks > 0);
+        mma_commit(bar(B_QKD));
+        ok = mbar_wait(bar(B_XRDY), x_at++ & 1, abort) && (t == 0 || mbar_wait(bar(B_OF), (t - 1) & 1, abort));
+        if (!ok) break;
+        tc_after();
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks)
+          mma(tmem + O2_COL, desc(q_lo + step_k(ks % (D / 16))), desc(x_lo + step_mn(ks)), idesc(false, true, D), ks > 0);
+        mma_commit(bar(B_EMPTY + rq.s));
+        ok = k_made() && landed(rv);
+        if (!ok) break;
+        tc_after();
+        dx(sbase + rk.s * SLOT, sbase + rv.s * SLOT, here(lo_at));
+        mma_commit(bar(B_EMPTY + rk.s));
+        ok = mbar_wait(bar(B_PRDY), t & 1, abort);
+        if (!ok) break;
+        tc_after();
+        // 16 tokens per step; rows of blocks of 32 that lie before them are left alone: a v that is not finite reaches
+        // no earlier block
+        const uint32_t v_lo = desc_lo(sbase + rv.s * SLOT, BOX);
+        if (!rev) {
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks)
+            mma_ts(tmem + O1_COL, tmem + SC_COL + 8u * ks, desc(v_lo + step_mn(ks)), idesc(false, true, D), ks > 0,
+                   ks >= 2 ? ~0u : 0u, ks >= 4 ? ~0u : 0u, ks >= 6 ? ~0u : 0u, 0u);
+        } else {
+#pragma unroll
+          for (int ks = 7; ks >= 0; --ks)
+            mma_ts(tmem + O1_COL, tmem + SC_COL + 8u * ks, desc(v_lo + step_mn(ks)), idesc(false, true, D), ks < 7, 0u,
+                   ks < 2 ? ~0u : 0u, ks < 4 ? ~0u : 0u, ks < 6 ? ~0u : 0u);
+        }
+        mma_commit(bar(B_OD));
+        mma_commit(bar(B_EMPTY + rv.s));
+        rk = rv.next();
+      }
+      if (!ok) {                                   // nothing of this block's may still run when its TMEM goes
+        mma_commit(bar(B_DRAIN));
+        mbar_wait(bar(B_DRAIN), 0, abort);
+      }
+    } else if (tid == (kMmaWarp + 1) * 32) {
+    // =============================== loads ===============================
+      int item = 0;
+      Ring<NSLOT> r;
+      bool ok = true;
+      auto load = [&](int m, int t) {
+        if (item >= NSLOT) ok = mbar_wait(bar(B_EMPTY + r.s), r.phase ^ 1u, abort);
+        if (!ok) return;
+        mbar_expect(bar(B_FULL + r.s), SLOT);
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x)
+          tma_load(sbase + r.s * SLOT + (uint32_t)x * BOX, &args.map[m], 64 * x, first(t), h * args.hmul[m], b * args.bmul[m], bar(B_FULL + r.s));
+        ++item;
+        r = r.next();
+      };
+    for (int t = 0; ok && t < ns; ++t) {
+      load(sw.mk, t);
+      if (ok) load(sw.mv, t);
+    }
+    for (int t = 0; ok && t < nt; ++t) {
+      load(sw.mk, t);
+      if (ok) load(sw.mq, t);
+      if (ok) load(sw.mv, t);
+    }
+    if (!ok || *abort)                             // what is on its way lands before the block leaves
+      for (int i = item > NSLOT ? item - NSLOT : 0; i < item; ++i) mbar_wait(bar(B_FULL + i % NSLOT), (i / NSLOT) & 1, abort);
+    }
+  }
+  __syncwarp();
+  tc_before();
+  __syncthreads();
+  if (tid == 0 && ctl.abort) report(status, LA_ERR_TIMEOUT);
+  if (nseg > 1) cluster_sync();                    // nobody reads this block's shared memory any more
+  if (warp == kMmaWarp) {
+    tc_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
+  }
+}
+
+// ---- host side ----
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static EncodeTiledFn encode_fn() {
+  static EncodeTiledFn fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return reinterpret_cast<EncodeTiledFn>(p);
+  }();
+  return fn;
+}
+// A view as [B, H, T, d]; an axis of stride 0 becomes one of a single element.  Rows outside 0 ... T - 1 read as zeros.
+static bool make_map(CUtensorMap* m, const la_view& v, int B, int H, int T, int d) {
+  cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)T, (cuuint64_t)(v.sh ? H : 1), (cuuint64_t)(v.sb ? B : 1)};
+  cuuint64_t strides[3] = {(cuuint64_t)v.st * 2, (cuuint64_t)(v.sh ? v.sh : v.st) * 2, (cuuint64_t)(v.sb ? v.sb : v.st) * 2};
+  cuuint32_t box[4] = {64, TILE, 1, 1}, es[4] = {1, 1, 1, 1};
+  return encode_fn()(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, v.p, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace dtc
+
+// Blocks per chain: one, unless the chains leave SMs idle and a chain is long enough that halving it (the sums of the
+// segments are formed first, so a token costs about 1.5 times as much) pays.
+static int segments(const la_ctx* ctx, int64_t chains, int tiles) {
+  int n = 1;
+  while (n < dtc::kMaxSeg / 2 && chains * n * 2 <= ctx->sm_count && tiles >= n * 4) n *= 2;
+  return n;
+}
+
+cudaError_t launch_decay_tc(la_ctx* ctx, int B, int T, const DecayPasses& ps, const float* log_decay, const int32_t* lens,
+                            int64_t* pos, cudaStream_t s, bool* handled) {
+  const la_config& c = ctx->cfg;
+  *handled = c.io_dtype == LA_BF16;
+  if (!*handled) return cudaSuccess;
+  if (!dtc::encode_fn()) return cudaErrorNotSupported;
+  dtc::Args a = {};
+  a.n = ps.n;
+  la_view seen[4];
+  int nmaps = 0;
+  auto map_of = [&](const la_view& v) {            // the sweeps share the tensors
+    for (int i = 0; i < nmaps; ++i)
+      if (seen[i].p == v.p && seen[i].sb == v.sb && seen[i].sh == v.sh && seen[i].st == v.st) return i;
+    if (!dtc::make_map(&a.map[nmaps], v, B, c.H, T, c.d)) return -1;
+    seen[nmaps] = v;
+    a.hmul[nmaps] = v.sh ? 1 : 0;
+    a.bmul[nmaps] = v.sb ? 1 : 0;
+    return nmaps++;
+  };
+  for (int i = 0; i < ps.n; ++i) {
+    const DecayPass& p = ps.p[i];
+    a.sw[i] = {p.o, p.S_in, p.S_out, p.r, p.upd, p.rev, p.trans, map_of(p.q), map_of(p.k), map_of(p.v)};
+    if (a.sw[i].mq < 0 || a.sw[i].mk < 0 || a.sw[i].mv < 0) return cudaErrorInvalidValue;
+  }
+  const int64_t chains = (int64_t)B * c.H * ps.n;
+  const int nseg = segments(ctx, chains, (T + dtc::TILE - 1) / dtc::TILE);
+  if (chains * nseg > INT32_MAX) return cudaErrorInvalidValue;
+  auto kern = c.d == 128 ? dtc::decay_tc_kernel<128> : dtc::decay_tc_kernel<64>;
+  const size_t smem = c.d == 128 ? dtc::smem_bytes<128>() : dtc::smem_bytes<64>();
+  cudaError_t e = allow_smem((const void*)kern, ctx->device);
+  if (e != cudaSuccess) return e;
+  ctx->launches += 1;
+  const int early = 2 * chains * nseg <= ctx->sm_count;
+  return launch_cluster(nseg, early, kern, dim3((unsigned)(chains * nseg)), dim3(dtc::kThreads), smem, s, a, log_decay, lens, pos,
+                        ctx->d_status, c.H, T, nseg, early);
+}
+
+}  // namespace la

@@ -72,6 +72,12 @@ bool norm_rope_args_ok(const la_ctx* ctx, const la_norm_rope_args* a) {
 // The sweeps of one call of the layer with a decay.
 la_status decay_sweeps(la_ctx* ctx, int B, int T, const la::DecayPasses& ps, const float* log_decay, const int32_t* lens,
                        int64_t* pos, cudaStream_t s) {
+  if (ctx->prefill_kernel == 0 && T > 16) {
+    bool handled = false;
+    const cudaError_t e = la::launch_decay_tc(ctx, B, T, ps, log_decay, lens, pos, s, &handled);
+    if (e != cudaSuccess) return cuda_status(e);
+    if (handled) return LA_OK;
+  }
   return cuda_status(la::launch_decay_walk(ctx, B, T, ps, log_decay, lens, pos, s));
 }
 

@@ -205,6 +205,9 @@ struct DecayPasses {
 };
 cudaError_t launch_decay_walk(la_ctx* ctx, int B, int T, const DecayPasses& ps, const float* log_decay, const int32_t* lens,
                               int64_t* pos, cudaStream_t s);
+// ... on the tensor cores (bf16 io).  Sets *handled to false when the type is not covered.
+cudaError_t launch_decay_tc(la_ctx* ctx, int B, int T, const DecayPasses& ps, const float* log_decay, const int32_t* lens,
+                            int64_t* pos, cudaStream_t s, bool* handled);
 cudaError_t launch_decay_step(la_ctx* ctx, int B, const la_view& q, const la_view& k, const la_view& v,
                               const float* log_decay, float scale, float* S, int64_t* pos, const la_view& o, cudaStream_t s);
 cudaError_t launch_norm_rope(la_ctx* ctx, int B, int T, const la_norm_rope_args& a, const la_view& q, const la_view& k,
