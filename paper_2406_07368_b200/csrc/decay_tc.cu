@@ -11,10 +11,11 @@
 //   dX = K~^T V           K~_j = upd lam^(n-1-j) k_j, as two bf16 numbers (hi + lo) per value
 // The state is fp32, and a user is handed it: k rounded to bf16 behind its factor would leave it 2^-9 off per term; hi + lo
 // is 2^-17 off and costs one more product, which the tensor cores have time for.  X itself stays in the registers of
-// 256 threads (X = lam^n X + dX), so that no tile waits for another one's accumulator.
+// 512 threads (X = lam^n X + dX), so that no tile waits for another one's accumulator.
 //
-// Roles, side by side: warps 0-3 mask P, warps 4-7 write the outputs, warps 8-15 hold X and make K~ and the bf16 copy of X,
-// one lane of warp 16 issues the products, one of warp 17 the TMA loads into a ring of tiles.
+// Roles, side by side: warps 0-7 mask P, warps 8-11 write the outputs, warps 12-27 hold X and make K~ and the bf16 copy of X,
+// one lane of warp 28 issues the products, one of warp 29 the TMA loads into a ring of tiles, one of warp 30 the stores of the
+// outputs, which are staged where the tile's V was.
 // No factor is formed as lam^i lam^-j, which overflows for heads that forget fast: 32 columns at a time share the exponent
 // of their nearest one, which is never negative, and the diagonal blocks take theirs from a table.
 // Few chains of a long sequence: a cluster of up to 16 blocks takes one chain, a segment each.  Every block first forms
@@ -29,10 +30,12 @@ namespace la {
 namespace dtc {
 
 constexpr int TILE = 128;
-constexpr int kThreadsA = 128, kThreadsB = 128, kThreadsC = 256, kMmaWarp = 16 /* its fellows 17 (loads), 18, 19 */, kThreads = 640;
-// Registers per thread once the roles have traded theirs: the launch gives everyone 96, per scheduler five warps of them.
-constexpr int kRegsA = 72, kRegsB = 88, kRegsC = 128, kRegsIssue = 64;
-static_assert(kRegsA + kRegsB + 2 * kRegsC + kRegsIssue == 5 * 96, "register split");
+constexpr int kThreadsA = 256, kThreadsB = 128, kThreadsC = 512, kThreads = 1024;
+constexpr int kWarpB = 8, kWarpC = 12, kMmaWarp = 28 /* its fellows 29 (loads), 30 (stores), 31 */;
+// Registers per thread once the roles have traded theirs: the launch gives everyone 64, per scheduler eight warps of them.
+// (No role may spill: nearly all of the SM's memory is shared memory, and a local load takes its way through the L2.)
+constexpr int kRegsA = 56, kRegsB = 64, kRegsC = 72, kRegsIssue = 48;
+static_assert(2 * kRegsA + kRegsB + 4 * kRegsC + kRegsIssue == 8 * 64, "register split");
 constexpr uint32_t BOX = 128 * 128;                // 128 rows x 64 bf16, 128-byte swizzle
 constexpr uint32_t SC_COL = 0, O1_COL = 128, O2_COL = 256, DX_COL = 384, TMEM_COLS = 512;
 constexpr int kMaxSeg = 16;
@@ -48,12 +51,15 @@ struct Ctl {
   float tab[64];                                   // 32 + x: r upd lam^|x| where column x of a diagonal block, counted from
                                                    // the row's own, is not later than the row, else 0
   float col[32];                                   // lam to the distance between column j and the nearest of its 32 columns
+  float kf[TILE];                                  // the factor of K~ in row i of a whole tile
+  Fade fade[3];                                    // lam^128; lam^n of the last tile, of n tokens; of the first of a sweep backwards
+                                                   // (which starts from the gradient as it is) lam^(n - 1)
   uint32_t tmem_base;
   int abort;
 };
 // KRDY and LO exist twice: the state pass makes K~ of a tile while the product of the one before runs.  Every other barrier
 // completes once per tile, and nobody completes it again before its waiters have passed.
-enum { B_FULL = 0, B_EMPTY = 10, B_QKD = 20, B_PRDY, B_KRDY0, B_KRDY1, B_DXD, B_XRDY, B_OD, B_OF, B_SHARED, B_TAKEN, B_DRAIN,
+enum { B_FULL = 0, B_EMPTY = 10, B_QKD = 20, B_PRDY, B_KRDY0, B_KRDY1, B_DXD, B_XRDY, B_QSD, B_OD, B_OF, B_STAGED, B_SHARED, B_TAKEN, B_DRAIN,
        kNumBars };
 static_assert(kNumBars <= 40, "Ctl::bars");
 template <int D> constexpr uint32_t smem_bytes() { return Map<D>::OFF_CTL + (uint32_t)sizeof(Ctl) + 1024u; }
@@ -106,7 +112,7 @@ __device__ __forceinline__ float4 ld_cluster(uint32_t addr) {
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
-__device__ __forceinline__ void sync_c() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+__device__ __forceinline__ void sync_c() { asm volatile("bar.sync 1, 512;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -115,6 +121,11 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, i
       "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
       ::"r"(dst), "l"(map), "r"(x), "r"(t), "r"(h), "r"(b), "r"(bar)
       : "memory");
+}
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, int x, int t, int h, int b, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%1, %2, %3, %4}], [%5];" ::"l"(map), "r"(x), "r"(t), "r"(h),
+               "r"(b), "r"(src)
+               : "memory");
 }
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
   asm volatile(
@@ -130,6 +141,29 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %6, %7, %8}, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc),
       "r"((uint32_t)acc), "r"(m0), "r"(m1), "r"(m2), "r"(m3)
       : "memory");
+}
+__device__ __forceinline__ uint64_t desc(uint32_t lo);
+// Products of N steps, rolled up but for two steps at a time: the code of all roles shares the instruction cache.
+// Q K^T: both contraction indices run along the 128-byte rows, 4 steps per box of 64.
+template <int N> __device__ __forceinline__ void product_kk(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
+#pragma unroll 1
+  for (int i = 0; i < N / 4; ++i, a += BOX >> 4, b += BOX >> 4)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) mma(d, desc(a + 2u * j), desc(b + 2u * j), idesc, i > 0 || j > 0);
+}
+// Q X: a along its rows (its N / 4 boxes as often as 8 steps need), b down the rows of its tile.
+template <int N> __device__ __forceinline__ void product_km(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
+#pragma unroll 1
+  for (int i = 0; i < 2; ++i, a += N > 4 ? BOX >> 4 : 0u, b += 512u)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) mma(d, desc(a + 2u * j), desc(b + 128u * j), idesc, i > 0 || j > 0);
+}
+// K~^T V: both down the rows.
+__device__ __forceinline__ void product_mm(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool acc) {
+#pragma unroll 1
+  for (int i = 0; i < 2; ++i, a += 512u, b += 512u)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) mma(d, desc(a + 128u * j), desc(b + 128u * j), idesc, acc || i > 0 || j > 0);
 }
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -154,12 +188,10 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
       : "r"(taddr)
       : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -171,10 +203,6 @@ __device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lbo) { retur
 __device__ __forceinline__ uint64_t desc(uint32_t lo) {
   return ((uint64_t)((1024u >> 4) | (1u << 14) | (2u << 29)) << 32) | lo;
 }
-// Step ks of 16 values where the contraction index runs along the 128-byte rows, ...
-__host__ __device__ constexpr uint32_t step_k(int ks) { return ((uint32_t)(ks >> 2) * BOX + (uint32_t)(ks & 3) * 32u) >> 4; }
-// ... or of 16 rows where it runs along the rows of the tile (the leading offset then leads to the next 64 columns).
-__host__ __device__ constexpr uint32_t step_mn(int ks) { return (uint32_t)ks * 2048u >> 4; }
 // bf16 x bf16 with fp32 sums, M = 128, N = n; a_mn, b_mn: that operand's contraction index runs along the rows of its tile.
 __host__ __device__ constexpr uint32_t idesc(bool a_mn, bool b_mn, uint32_t n) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
@@ -185,6 +213,10 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
+// (two fp32 numbers per instruction; each half rounds as the scalar one does)
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ uint32_t pack2(float2 v) { return pack2(v.x, v.y); }
 __device__ __forceinline__ float lo_f(uint32_t u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float hi_f(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
 // (volatile: read where they are used, tile after tile, instead of kept in 32 registers)
@@ -227,7 +259,7 @@ struct Sweep {
   int mq, mk, mv;                                  // which tensor maps
 };
 struct alignas(64) Args {
-  CUtensorMap map[4];
+  CUtensorMap map[4], out[3];
   int hmul[4], bmul[4];                            // 0: the tensor is broadcast over heads / sequences
   Sweep sw[3];
   int n;
@@ -239,7 +271,7 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
                 int64_t* __restrict__ pos, int* status, int H, int Tlen, int nseg, int early) {
   using M = Map<D>;
   constexpr uint32_t SLOT = M::SLOT;
-  constexpr int NSLOT = M::NSLOT, NX = D / 2;      // NX: values of X per thread of group C
+  constexpr int NSLOT = M::NSLOT, NX = D / 4;      // NX: values of X per thread of group C
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* smem = smem_dyn + ((1024u - (smem_u32(smem_dyn) & 1023u)) & 1023u);
   const uint32_t sbase = smem_u32(smem);
@@ -264,8 +296,10 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
     mbar_init(bar(B_KRDY1), kThreadsC);
     mbar_init(bar(B_DXD), 1);
     mbar_init(bar(B_XRDY), kThreadsC);
+    mbar_init(bar(B_QSD), 1);
     mbar_init(bar(B_OD), 1);
     mbar_init(bar(B_OF), kThreadsB);
+    mbar_init(bar(B_STAGED), kThreadsB);
     mbar_init(bar(B_SHARED), rank > 0 ? rank : 1);                 // from every block before this one
     mbar_init(bar(B_TAKEN), rank < nseg - 1 ? nseg - 1 - rank : 1);  // from every block behind it
     mbar_init(bar(B_DRAIN), 1);
@@ -281,11 +315,22 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
   const float g = log_decay[h];
   const int L = seq_len(lens, b, Tlen);
   const bool bad = L < 0 || !decay_ok(g);
+  // Tokens n0 ... n1 - 1 of the sweep are this block's, in whole tiles but for the sequence's last one.
+  const int rev = sw.rev;
+  const int tiles_all = bad ? 0 : (L + TILE - 1) / TILE, seg = (tiles_all + nseg - 1) / nseg * TILE;
+  const int n0 = min(L, rank * seg), n1 = min(L, n0 + seg);
+  const int nt = bad ? 0 : (n1 - n0 + TILE - 1) / TILE;
+  const int ns = nseg > 1 && rank < nseg - 1 ? nt : 0;             // tiles of the state pass
+  if (tid >= 96 && tid < 99) {
+    const int n = (n1 - n0 + TILE - 1) % TILE + 1;
+    ctl.fade[tid - 96] = decay_fade(bad ? 0.f : g, tid == 96 ? TILE : tid == 97 ? n : min(TILE, max(n1 - n0, 1)) - 1);
+  }
   if (tid >= 64 && tid < 96) ctl.col[lane] = bad ? 0.f : decay_pow(g, sw.rev ? lane : 31 - lane);
   if (tid < 64) {
     const int x = sw.rev ? tid - 32 : 32 - tid;
     ctl.tab[tid] = x < 0 || bad ? 0.f : sw.r * sw.upd * decay_pow(g, x);
   }
+  if (tid >= 128 && tid < 128 + TILE) ctl.kf[tid - 128] = bad ? 0.f : sw.upd * decay_pow(g, sw.rev ? tid - 128 : TILE - 1 - (tid - 128));
   tc_before();
   __syncthreads();
   tc_after();
@@ -294,79 +339,82 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
   if (pos && L > 0 && chain % args.n == 0 && rank == 0 && h == 0 && tid == 0) pos[b] += L;
   if (bad && tid == 0) report(status, LA_ERR_INVALID_ARG);
 
-  // Tokens n0 ... n1 - 1 of the sweep are this block's, in whole tiles but for the sequence's last one.
-  const int rev = sw.rev;
-  const int tiles_all = bad ? 0 : (L + TILE - 1) / TILE, seg = (tiles_all + nseg - 1) / nseg * TILE;
-  const int n0 = min(L, rank * seg), n1 = min(L, n0 + seg);
-  const int nt = bad ? 0 : (n1 - n0 + TILE - 1) / TILE;
-  const int ns = nseg > 1 && rank < nseg - 1 ? nt : 0;             // tiles of the state pass
   auto count = [&](int t) { return min(TILE, n1 - n0 - t * TILE); };   // tokens of tile t
   auto first = [&](int t) {                        // token in row 0 (backwards: may be negative, those rows read as zeros)
     const int s = n0 + t * TILE;
     return rev ? L - s - TILE : s;
   };
 
-  if (warp < 4) {
+  if (warp < kWarpB) {
     // =============================== group A: P -> P o M ===============================
     regs_down<kRegsA>();
+    const int q4 = warp & 3, c0 = warp >> 2 << 1;  // rows 32 q4 ..., blocks of 32 columns c0, c0 + 1
     float base[3];
 #pragma unroll
     for (int i = 0; i < 3; ++i) base[i] = bad ? 0.f : sw.r * sw.upd * decay_pow(g, rev ? 32 * (i + 1) - lane : 32 * (i + 1) - 31 + lane);
     const uint32_t diag = smem_u32(ctl.tab + 32) - 4u * (uint32_t)lane, col = smem_u32(ctl.col);
     const uint32_t seen_cols = rev ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);   // of the diagonal block
-    const uint32_t t0 = tmem + SC_COL + ((uint32_t)(warp * 32) << 16);
+    // P o M of columns 64 i ... 64 i + 63 goes to columns 64 i ... 64 i + 31: over columns that the same thread has read
+    const uint32_t t0 = tmem + SC_COL + ((uint32_t)(q4 * 32) << 16) + 32u * c0;
     for (int t = 0; t < nt; ++t) {
       if (!warp_wait(bar(B_QKD), t & 1, abort)) break;
       tc_after();
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {                // 32 columns; this warp's rows meet them all, in part or not at all
-        const int ahead = rev ? c - warp : warp - c;
-        uint32_t p[16];
+#pragma unroll 1
+      for (int c = 0; c < 2; ++c) {                // this warp's rows meet the 32 columns all, in part or not at all
+        const int ahead = rev ? c0 + c - q4 : q4 - c0 - c;
         if (ahead < 0) {
+          const uint32_t p[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+          tmem_st8(t0 + 16u * c, p);
+          tmem_st8(t0 + 16u * c + 8u, p);
+          continue;
+        }
+        const uint32_t m = here(seen_cols);
+        const float f = ahead == 1 ? base[0] : ahead == 2 ? base[1] : base[2];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) p[j] = 0u;
-        } else {
-          uint32_t s[32];
-          tmem_ld32(t0 + 32u * c, s);
+        for (int i = 0; i < 32; i += 16) {
+          uint32_t s[16], p[8];
+          tmem_ld16(t0 + 32u * c + i, s);
           tmem_wait_ld();
           if (ahead == 0) {
-            const uint32_t m = here(seen_cols);
-            // (a select: behind the diagonal a score that is not finite must not meet the factor 0)
+            // (masked as bits: behind the diagonal the factor 0 would leave a NaN of a score that is not finite)
 #pragma unroll
-            for (int j = 0; j < 32; j += 2)
-              p[j / 2] = pack2(m >> j & 1u ? asf(s[j]) * lds(diag + 4u * j) : 0.f, m >> (j + 1) & 1u ? asf(s[j + 1]) * lds(diag + 4u * (j + 1)) : 0.f);
+            for (int j = 0; j < 16; j += 2)
+              p[j / 2] = pack2(mul2(make_float2(asf(s[j]), asf(s[j + 1])), make_float2(lds(diag + 4u * (i + j)), lds(diag + 4u * (i + j + 1))))) &
+                         ((m >> (i + j) & 1u ? 0xffffu : 0u) | (m >> (i + j + 1) & 1u ? 0xffff0000u : 0u));
           } else {
-            const float f = ahead == 1 ? base[0] : ahead == 2 ? base[1] : base[2];
 #pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-              const float4 w = lds4(col + 4u * j);
-              p[j / 2] = pack2(asf(s[j]) * (f * w.x), asf(s[j + 1]) * (f * w.y));
-              p[j / 2 + 1] = pack2(asf(s[j + 2]) * (f * w.z), asf(s[j + 3]) * (f * w.w));
+            for (int j = 0; j < 16; j += 4) {
+              const float4 w = lds4(col + 4u * (i + j));
+              p[j / 2] = pack2(mul2(make_float2(asf(s[j]), asf(s[j + 1])), mul2(make_float2(f, f), make_float2(w.x, w.y))));
+              p[j / 2 + 1] = pack2(mul2(make_float2(asf(s[j + 2]), asf(s[j + 3])), mul2(make_float2(f, f), make_float2(w.z, w.w))));
             }
           }
+          tmem_st8(t0 + 16u * c + i / 2, p);
         }
-        tmem_st16(t0 + 16u * c, p);                // over columns of its own rows that have been read
       }
       tmem_wait_st();
       tc_before();
       mbar_arrive(bar(B_PRDY));
     }
-  } else if (warp < 8) {
+  } else if (warp < kWarpC) {
     // =============================== group B: outputs ===============================
-    regs_down<kRegsB>();
-    const int row = (warp - 4) * 32 + lane, age = rev ? TILE - 1 - row : row;
-    const uint32_t tl = tmem + ((uint32_t)((warp - 4) * 32) << 16);
+    const int row = (warp - kWarpB) * 32 + lane, age = rev ? TILE - 1 - row : row;
+    const uint32_t tl = tmem + ((uint32_t)((warp - kWarpB) * 32) << 16);
     __nv_bfloat16* o = (__nv_bfloat16*)sw.o.p + b * sw.o.sb + h * sw.o.sh;
     const float f_all = bad ? 0.f : sw.r * decay_pow(g, age + 1), f_first = bad ? 0.f : sw.r * decay_pow(g, age);
+    const uint32_t r_at = row_at(row);
+    Ring<NSLOT> ring;                              // of V of the tile: its place takes the outputs, which TMA stores
+    for (int i = 0; i < 2 * ns + 2; ++i) ring = ring.next();
     for (int t = 0; t < nt; ++t) {
       if (!warp_wait(bar(B_OD), t & 1, abort)) break;
       tc_after();
       const float f = rev && n0 + t == 0 ? f_first : f_all;        // (a sweep backwards starts from the gradient as it is)
-      const bool live = age < count(t);
+      const int n = count(t);
       __nv_bfloat16* to = o + (int64_t)(first(t) + row) * sw.o.st;
-#pragma unroll
+      const uint32_t at = sbase + ring.s * SLOT + r_at;
+#pragma unroll 1
       for (int c = 0; c < D / 16; ++c) {
-        uint32_t x[16], y[16];
+        uint32_t x[16], y[16], w[8];
         tmem_ld16(tl + O1_COL + 16u * c, x);
         tmem_ld16(tl + O2_COL + 16u * c, y);
         tmem_wait_ld();
@@ -374,64 +422,87 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
           tc_before();
           mbar_arrive(bar(B_OF));
         }
-        if (live) {
-          uint32_t w[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) w[i] = pack2(fmaf(f, asf(y[2 * i]), asf(x[2 * i])), fmaf(f, asf(y[2 * i + 1]), asf(x[2 * i + 1])));
+        for (int i = 0; i < 8; ++i)
+          w[i] = pack2(fma2(make_float2(f, f), make_float2(asf(y[2 * i]), asf(y[2 * i + 1])), make_float2(asf(x[2 * i]), asf(x[2 * i + 1]))));
+        if (n == TILE) {
+          const uint32_t p = (at ^ (32u * (c & 3))) + (D == 128 ? (uint32_t)(c >> 2) * BOX : 0u);
+          sts128(p, w[0], w[1], w[2], w[3]);
+          sts128(p ^ 16u, w[4], w[5], w[6], w[7]);
+        } else if (age < n) {                      // (a tile in part: its rows one by one)
           *reinterpret_cast<uint4*>(to + 16 * c) = make_uint4(w[0], w[1], w[2], w[3]);
           *reinterpret_cast<uint4*>(to + 16 * c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
         }
       }
+      fence_async();
+      mbar_arrive(bar(B_STAGED));
+      ring = ring.next().next().next();
     }
     if (!bad)                                      // rows behind the sequence
-      for (int64_t i = (int64_t)L * (D / 8) + rank * kThreadsB + (tid - 128); i < (int64_t)Tlen * (D / 8); i += (int64_t)nseg * kThreadsB)
+      for (int64_t i = (int64_t)L * (D / 8) + rank * kThreadsB + (tid - 32 * kWarpB); i < (int64_t)Tlen * (D / 8); i += (int64_t)nseg * kThreadsB)
         *reinterpret_cast<uint4*>(o + i / (D / 8) * sw.o.st + i % (D / 8) * 8) = make_uint4(0u, 0u, 0u, 0u);
-  } else if (warp < 16) {
+  } else if (warp < kMmaWarp) {
     // =============================== group C: X, K~, X as bf16 ===============================
     regs_up<kRegsC>();
-    const int ct = tid - 256, q4 = warp & 3, hf = (warp - 8) >> 2, a = 32 * q4 + lane;   // row a of X, columns hf NX ...
-    const int krow = ct & 127, kage = rev ? TILE - 1 - krow : krow, kh = ct >> 7;        // a row and a half of a tile
+    const int ct = tid - 32 * kWarpC, q4 = warp & 3, hf = (warp - kWarpC) >> 2, a = 32 * q4 + lane;   // row a of X, columns hf NX ...
+    const int krow = ct & 127, kage = rev ? TILE - 1 - krow : krow, kh = ct >> 7;        // a row and a quarter of a tile
     const uint32_t tx = tmem + DX_COL + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(hf * NX);
     const bool real = D == 128 || q4 < 2;          // d = 64: rows 64 ... hold the part of X that comes from lo
-    const size_t sat = ((size_t)bh * D + a) * D + hf * NX;
-    // (d = 64: the second half of a row starts at its piece 4)
-    const uint32_t k_at = D == 128 ? (uint32_t)kh * BOX + row_at(krow) : row_at(krow) ^ (64u * kh);
-    const uint32_t x_at = D == 128 ? (uint32_t)hf * BOX + row_at(a) : row_at(a) ^ (64u * hf);
+    auto sat = [&] { return ((size_t)here(bh) * D + here(a)) * D + here(hf) * NX; };   // (rarely wanted: not kept)
+    // Quarter i of a row: four pieces from piece 4 (i & 1) on of box i >> 1, or (d = 64) two pieces from 2 i on.
+    auto quarter = [&](int row, int i) {
+      return D == 128 ? (uint32_t)(i >> 1) * BOX + (row_at(row) ^ (64u * (i & 1))) : row_at(row) ^ (32u * i);
+    };
+    const uint32_t k_at = quarter(krow, kh), x_at = quarter(a, hf);
     float X[NX];
 #pragma unroll
     for (int i = 0; i < NX; ++i) X[i] = 0.f;
-    const float k_full = bad ? 0.f : sw.upd * decay_pow(g, TILE - 1 - kage);
-    const Fade fade_full = decay_fade(bad ? 0.f : g, TILE);
+    const uint32_t kf_at = smem_u32(ctl.kf) + 4u * krow, fade_at = smem_u32(ctl.fade);
     Ring<NSLOT> ring;
     uint32_t made = 0, seen = 0;                   // tiles of K~ made, products dX waited for
     bool ok = true;
 
     // K~ of a tile: hi in the place of K, lo beside it.  Rows without a token are zeros in K~ and (they may hold anything
-    // where the sequence is shorter than the tensor) in V.
-    auto make_k = [&](Ring<NSLOT> rk, Ring<NSLOT> rv, int n, uint32_t lo_at) -> bool {
+    // where the sequence is shorter than the tensor) in V.  First what needs only K to have landed; hi stays in registers
+    // until Q K^T has read K as it is.
+    uint32_t hi[D / 8];
+    auto split_k = [&](const Ring<NSLOT>& rk, int n, uint32_t lo_at) -> bool {
       if (!warp_wait(bar(B_FULL + rk.s), rk.phase, abort)) return false;
       const uint32_t at = sbase + here(k_at), kp = at + rk.s * SLOT, lp = at + lo_at;
       const bool live = kage < n;
-      const float f = n == TILE ? k_full : live ? sw.upd * decay_pow(g, n - 1 - kage) : 0.f;
+      const float f1 = live ? lds(kf_at + (rev ? -4 : 4) * (TILE - n)) : 0.f;   // (a tile of n tokens: the last n factors)
+      const float2 f = make_float2(f1, f1);
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
+      for (int i = 0; i < D / 32; ++i) {
         const uint4 u = lds128(kp ^ (16u * i));
-        const uint32_t in[4] = {u.x, u.y, u.z, u.w};
-        uint32_t hi[4], lo[4];
+        hi[4 * i] = u.x, hi[4 * i + 1] = u.y, hi[4 * i + 2] = u.z, hi[4 * i + 3] = u.w;
+      }
+      if (!live)
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) hi[i] = 0u;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        uint32_t lo[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float x = lo_f(in[j]), y = hi_f(in[j]);
-          hi[j] = live ? pack2(x * f, y * f) : 0u;
-          lo[j] = live ? pack2(fmaf(x, f, -lo_f(hi[j])), fmaf(y, f, -hi_f(hi[j]))) : 0u;
+          const uint32_t u = hi[4 * i + j];
+          const float2 x = mul2(make_float2(lo_f(u), hi_f(u)), f);
+          const uint32_t w = hi[4 * i + j] = pack2(x);
+          lo[j] = pack2(fma2(make_float2(lo_f(w), hi_f(w)), make_float2(-1.f, -1.f), x));
         }
-        sts128(kp ^ (16u * i), hi[0], hi[1], hi[2], hi[3]);
         sts128(lp ^ (16u * i), lo[0], lo[1], lo[2], lo[3]);
       }
+      return true;
+    };
+    auto put_k = [&](const Ring<NSLOT>& rk, const Ring<NSLOT>& rv, int n) -> bool {
+      const uint32_t at = sbase + here(k_at), kp = at + rk.s * SLOT;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) sts128(kp ^ (16u * i), hi[4 * i], hi[4 * i + 1], hi[4 * i + 2], hi[4 * i + 3]);
       if (n < TILE) {
         if (!warp_wait(bar(B_FULL + rv.s), rv.phase, abort)) return false;
-        if (!live) {
+        if (kage >= n) {
 #pragma unroll
-          for (int i = 0; i < D / 16; ++i) sts128((at + rv.s * SLOT) ^ (16u * i), 0u, 0u, 0u, 0u);
+          for (int i = 0; i < D / 32; ++i) sts128((at + rv.s * SLOT) ^ (16u * i), 0u, 0u, 0u, 0u);
         }
       }
       fence_async();
@@ -440,17 +511,22 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
       return true;
     };
     // X = lam^n X + dX
-    auto take_dx = [&](const Fade& f) -> bool {
+    auto take_dx = [&](uint32_t i) -> bool {
       if (!warp_wait(bar(B_DXD), seen & 1, abort)) return false;
       ++seen;
       tc_after();
+      const Fade f = {lds(fade_at + 8u * i), lds(fade_at + 8u * i + 4u)};
 #pragma unroll
-      for (int c = 0; c < NX / 32; ++c) {
-        uint32_t x[32];
-        tmem_ld32(tx + 32u * c, x);
+      for (int c = 0; c < NX; c += 16) {
+        uint32_t x[16];
+        tmem_ld16(tx + c, x);
         tmem_wait_ld();
 #pragma unroll
-        for (int j = 0; j < 32; ++j) X[32 * c + j] = f(X[32 * c + j]) + asf(x[j]);
+        for (int j = 0; j < 16; j += 2) {
+          const float2 y = make_float2(X[c + j], X[c + j + 1]);
+          const float2 s = fma2(make_float2(f.hi, f.hi), y, fma2(make_float2(f.lo, f.lo), y, make_float2(asf(x[j]), asf(x[j + 1]))));
+          X[c + j] = s.x, X[c + j + 1] = s.y;
+        }
       }
       tc_before();
       return true;
@@ -466,12 +542,13 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
 
     if (nseg > 1) {                                // (a bad head's blocks pass through with zeros and write nothing)
       // the sum of this block's segment, from nothing
-      if (ns > 0) ok = make_k(ring, ring.next(), count(0), M::OFF_LO);
-      for (int t = 0; ok && t < ns; ++t) {
+      int left = rank < nseg - 1 ? n1 - n0 : 0;
+      if (left > 0) ok = split_k(ring, min(TILE, left), M::OFF_LO) && put_k(ring, ring.next(), min(TILE, left));
+      for (uint32_t lo_at = M::OFF_X; ok && left > 0; left -= TILE, lo_at ^= M::OFF_X ^ M::OFF_LO) {
         ring = ring.next().next();
-        if (t + 1 < ns) ok = make_k(ring, ring.next(), count(t + 1), t & 1 ? M::OFF_LO : M::OFF_X);
-        if (!ok || !take_dx(count(t) == TILE ? fade_full : decay_fade(g, count(t)))) { ok = false; break; }
-        mbar_arrive(bar(B_XRDY));
+        if (left > TILE) ok = split_k(ring, min(TILE, left - TILE), lo_at) && put_k(ring, ring.next(), min(TILE, left - TILE));
+        ok = ok && take_dx(left < TILE);
+        if (ok) mbar_arrive(bar(B_XRDY));
       }
       if (rank < nseg - 1) {
 #pragma unroll
@@ -488,13 +565,13 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
     // X before the segment: the caller's state, then the sums of the segments before this one
     if (sw.S_in && real && !bad) {
       if (sw.trans) {
-        const float* p = sw.S_in + ((size_t)bh * D + hf * NX) * D + a;
+        const float* p = sw.S_in + ((size_t)here(bh) * D + here(hf) * NX) * D + a;
 #pragma unroll
         for (int i = 0; i < NX; ++i) X[i] = p[(size_t)i * D];
       } else {
 #pragma unroll
         for (int i = 0; i < NX; i += 4) {
-          const float4 v = *reinterpret_cast<const float4*>(sw.S_in + sat + i);
+          const float4 v = *reinterpret_cast<const float4*>(sw.S_in + sat() + i);
           X[i] = v.x, X[i + 1] = v.y, X[i + 2] = v.z, X[i + 3] = v.w;
         }
       }
@@ -516,6 +593,8 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
             X[4 * i + 1] = f(X[4 * i + 1]) + v.y;
             X[4 * i + 2] = f(X[4 * i + 2]) + v.z;
             X[4 * i + 3] = f(X[4 * i + 3]) + v.w;
+            if (i % 4 == 3)                        // (four loads in flight: more would not fit the registers)
+              asm volatile("" : "+f"(X[4 * i - 12]), "+f"(X[4 * i - 8]), "+f"(X[4 * i - 4]), "+f"(X[4 * i]));
           }
         }
         sync_c();
@@ -524,17 +603,20 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
       }
       if (rank < nseg - 1) ok = __all_sync(0xffffffffu, mbar_wait_cluster(bar(B_TAKEN), 0, abort)) && ok;
     }
-    if (ok && nt > 0) {
+    int left = bad ? 0 : n1 - n0, e = rev && n0 == 0;      // (a sweep backwards starts from the gradient as it is)
+    if (ok && left > 0) {
       write_x();
       mbar_arrive(bar(B_XRDY));
     }
-    for (int t = 0; ok && t < nt; ++t) {
-      const int n = count(t), e = rev && n0 + t == 0;
-      ok = warp_wait(bar(B_QKD), t & 1, abort);    // K has been read as it is
-      if (!ok || !make_k(ring, ring.next().next(), n, M::OFF_LO)) { ok = false; break; }
+    for (uint32_t qk = 0; ok && left > 0; left -= TILE, qk ^= 1u) {
+      const int n = min(TILE, left);
+      ok = split_k(ring, n, M::OFF_LO) && warp_wait(bar(B_QKD), qk, abort) && put_k(ring, ring.next().next(), n) && take_dx(e ? 2u : n < TILE);
+      if (!ok) break;
       ring = ring.next().next().next();
-      if (!take_dx(n == TILE && !e ? fade_full : decay_fade(g, n - e))) { ok = false; break; }
-      if (t + 1 < nt) {
+      e = 0;
+      if (left > TILE) {
+        ok = warp_wait(bar(B_QSD), qk, abort);     // Q X has read the copy before
+        if (!ok) break;
         write_x();
         mbar_arrive(bar(B_XRDY));
       }
@@ -545,20 +627,20 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
         if (!real)
 #pragma unroll
           for (int i = 0; i < NX / 4; ++i)
-            *reinterpret_cast<float4*>(smem + M::OFF_LO + (uint32_t)((i * 2 + hf) * 64 + a - 64) * 16u) =
+            *reinterpret_cast<float4*>(smem + M::OFF_LO + (uint32_t)((i * 4 + hf) * 64 + a - 64) * 16u) =
                 make_float4(X[4 * i], X[4 * i + 1], X[4 * i + 2], X[4 * i + 3]);
         sync_c();
         if (real)
 #pragma unroll
           for (int i = 0; i < NX / 4; ++i) {
-            const float4 v = *reinterpret_cast<const float4*>(smem + M::OFF_LO + (uint32_t)((i * 2 + hf) * 64 + a) * 16u);
+            const float4 v = *reinterpret_cast<const float4*>(smem + M::OFF_LO + (uint32_t)((i * 4 + hf) * 64 + a) * 16u);
             X[4 * i] += v.x, X[4 * i + 1] += v.y, X[4 * i + 2] += v.z, X[4 * i + 3] += v.w;
           }
       }
       if (real && ok)
 #pragma unroll
         for (int i = 0; i < NX; i += 4)
-          *reinterpret_cast<float4*>(sw.S_out + sat + i) = make_float4(f(X[i]), f(X[i + 1]), f(X[i + 2]), f(X[i + 3]));
+          *reinterpret_cast<float4*>(sw.S_out + sat() + i) = make_float4(f(X[i]), f(X[i + 1]), f(X[i + 2]), f(X[i + 3]));
     }
   } else {
     regs_down<kRegsIssue>();
@@ -576,15 +658,10 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
       auto dx = [&](uint32_t kt, uint32_t vt, uint32_t lo) {
         const uint32_t v_lo = desc_lo(vt, BOX);
         if (D == 128) {
-          const uint32_t hi_d = desc_lo(kt, BOX), lo_d = desc_lo(lo, BOX);
-#pragma unroll
-          for (int ks = 0; ks < 8; ++ks) mma(tmem + DX_COL, desc(hi_d + step_mn(ks)), desc(v_lo + step_mn(ks)), idesc(true, true, 128), ks > 0);
-#pragma unroll
-          for (int ks = 0; ks < 8; ++ks) mma(tmem + DX_COL, desc(lo_d + step_mn(ks)), desc(v_lo + step_mn(ks)), idesc(true, true, 128), true);
+          product_mm(tmem + DX_COL, desc_lo(kt, BOX), v_lo, idesc(true, true, 128), false);
+          product_mm(tmem + DX_COL, desc_lo(lo, BOX), v_lo, idesc(true, true, 128), true);
         } else {                                   // hi and lo side by side: rows 0-63 and 64-127 of one product
-          const uint32_t k_d = desc_lo(kt, lo - kt);
-#pragma unroll
-          for (int ks = 0; ks < 8; ++ks) mma(tmem + DX_COL, desc(k_d + step_mn(ks)), desc(v_lo + step_mn(ks)), idesc(true, true, 64), ks > 0);
+          product_mm(tmem + DX_COL, desc_lo(kt, lo - kt), v_lo, idesc(true, true, 64), false);
         }
         mma_commit(bar(B_DXD));
       };
@@ -606,40 +683,38 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
         ok = landed(rk) && landed(rq);
         if (!ok) break;
         tc_after();
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) mma(tmem + SC_COL, desc(q_lo + step_k(ks)), desc(k_lo + step_k(ks)), idesc(false, false, 128), ks > 0);
+        product_kk<D / 16>(tmem + SC_COL, q_lo, k_lo, idesc(false, false, 128));
         mma_commit(bar(B_QKD));
-        ok = mbar_wait(bar(B_XRDY), x_at++ & 1, abort) && (t == 0 || mbar_wait(bar(B_OF), (t - 1) & 1, abort));
-        if (!ok) break;
-        tc_after();
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks)
-          mma(tmem + O2_COL, desc(q_lo + step_k(ks % (D / 16))), desc(x_lo + step_mn(ks)), idesc(false, true, D), ks > 0);
-        mma_commit(bar(B_EMPTY + rq.s));
-        ok = k_made() && landed(rv);
+        ok = k_made() && landed(rv);               // (K~ of this tile: the sum of the tile before has been read)
         if (!ok) break;
         tc_after();
         dx(sbase + rk.s * SLOT, sbase + rv.s * SLOT, here(lo_at));
         mma_commit(bar(B_EMPTY + rk.s));
+        ok = mbar_wait(bar(B_XRDY), x_at++ & 1, abort) && (t == 0 || mbar_wait(bar(B_OF), (t - 1) & 1, abort));
+        if (!ok) break;
+        tc_after();
+        product_km<D / 16>(tmem + O2_COL, q_lo, x_lo, idesc(false, true, D));
+        mma_commit(bar(B_QSD));
+        mma_commit(bar(B_EMPTY + rq.s));
         ok = mbar_wait(bar(B_PRDY), t & 1, abort);
         if (!ok) break;
         tc_after();
         // 16 tokens per step; rows of blocks of 32 that lie before them are left alone: a v that is not finite reaches
         // no earlier block
         const uint32_t v_lo = desc_lo(sbase + rv.s * SLOT, BOX);
+        // (The masks as constants, a copy of the code per direction: as numbers of the run the product took twice as long.)
         if (!rev) {
 #pragma unroll
           for (int ks = 0; ks < 8; ++ks)
-            mma_ts(tmem + O1_COL, tmem + SC_COL + 8u * ks, desc(v_lo + step_mn(ks)), idesc(false, true, D), ks > 0,
+            mma_ts(tmem + O1_COL, tmem + SC_COL + 8u * ks + (ks < 4 ? 0u : 32u), desc(v_lo + 128u * ks), idesc(false, true, D), ks > 0,
                    ks >= 2 ? ~0u : 0u, ks >= 4 ? ~0u : 0u, ks >= 6 ? ~0u : 0u, 0u);
         } else {
 #pragma unroll
           for (int ks = 7; ks >= 0; --ks)
-            mma_ts(tmem + O1_COL, tmem + SC_COL + 8u * ks, desc(v_lo + step_mn(ks)), idesc(false, true, D), ks < 7, 0u,
+            mma_ts(tmem + O1_COL, tmem + SC_COL + 8u * ks + (ks < 4 ? 0u : 32u), desc(v_lo + 128u * ks), idesc(false, true, D), ks < 7, 0u,
                    ks < 2 ? ~0u : 0u, ks < 4 ? ~0u : 0u, ks < 6 ? ~0u : 0u);
         }
         mma_commit(bar(B_OD));
-        mma_commit(bar(B_EMPTY + rv.s));
         rk = rv.next();
       }
       if (!ok) {                                   // nothing of this block's may still run when its TMEM goes
@@ -672,6 +747,20 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
     }
     if (!ok || *abort)                             // what is on its way lands before the block leaves
       for (int i = item > NSLOT ? item - NSLOT : 0; i < item; ++i) mbar_wait(bar(B_FULL + i % NSLOT), (i / NSLOT) & 1, abort);
+    } else if (tid == (kMmaWarp + 2) * 32) {
+      // =============================== output stores ===============================
+      Ring<NSLOT> r;
+      for (int i = 0; i < 2 * ns + 2; ++i) r = r.next();
+      for (int t = 0; t < nt && count(t) == TILE; ++t) {
+        if (!mbar_wait(bar(B_STAGED), t & 1, abort)) break;
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x) tma_store(&args.out[chain % args.n], 64 * x, first(t), h, b, sbase + r.s * SLOT + (uint32_t)x * BOX);
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        mbar_arrive(bar(B_EMPTY + r.s));
+        r = r.next().next().next();
+      }
+      asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
   }
   __syncwarp();
@@ -740,7 +829,7 @@ cudaError_t launch_decay_tc(la_ctx* ctx, int B, int T, const DecayPasses& ps, co
   for (int i = 0; i < ps.n; ++i) {
     const DecayPass& p = ps.p[i];
     a.sw[i] = {p.o, p.S_in, p.S_out, p.r, p.upd, p.rev, p.trans, map_of(p.q), map_of(p.k), map_of(p.v)};
-    if (a.sw[i].mq < 0 || a.sw[i].mk < 0 || a.sw[i].mv < 0) return cudaErrorInvalidValue;
+    if (a.sw[i].mq < 0 || a.sw[i].mk < 0 || a.sw[i].mv < 0 || !dtc::make_map(&a.out[i], p.o, B, c.H, T, c.d)) return cudaErrorInvalidValue;
   }
   const int64_t chains = (int64_t)B * c.H * ps.n;
   const int nseg = segments(ctx, chains, (T + dtc::TILE - 1) / dtc::TILE);
