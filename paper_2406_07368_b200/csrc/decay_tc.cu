@@ -40,11 +40,11 @@ constexpr uint32_t BOX = 128 * 128;                // 128 rows x 64 bf16, 128-by
 constexpr uint32_t SC_COL = 0, O1_COL = 128, O2_COL = 256, DX_COL = 384, TMEM_COLS = 512;
 constexpr int kMaxSeg = 16;
 
-template <int D> struct Map {
+template <int D, bool LO> struct Map {
   static constexpr uint32_t SLOT = D / 64 * BOX;   // a tile of q, k or v
-  static constexpr int NSLOT = D == 128 ? 5 : 9;
+  static constexpr int NSLOT = D == 64 ? 9 : LO ? 5 : 6;
   // lo behind the ring; X as bf16: 128 rows (d = 64: rows 0-63 the part of X from hi, 64-127 that from lo)
-  static constexpr uint32_t OFF_LO = NSLOT * SLOT, OFF_X = OFF_LO + SLOT, OFF_CTL = OFF_X + SLOT;
+  static constexpr uint32_t OFF_LO = NSLOT * SLOT, OFF_X = OFF_LO + (LO ? SLOT : 0u), OFF_CTL = OFF_X + SLOT;
 };
 struct Ctl {
   unsigned long long bars[40];
@@ -62,9 +62,9 @@ struct Ctl {
 enum { B_FULL = 0, B_EMPTY = 10, B_QKD = 20, B_PRDY, B_KRDY0, B_KRDY1, B_DXD, B_XRDY, B_QSD, B_OD, B_OF, B_STAGED, B_SHARED, B_TAKEN, B_DRAIN,
        kNumBars };
 static_assert(kNumBars <= 40, "Ctl::bars");
-template <int D> constexpr uint32_t smem_bytes() { return Map<D>::OFF_CTL + (uint32_t)sizeof(Ctl) + 1024u; }
-static_assert(smem_bytes<128>() <= 227u * 1024u && smem_bytes<64>() <= 227u * 1024u, "shared memory");
-static_assert(smem_bytes<64>() > 114u * 1024u, "one block per SM: each allocates all of the TMEM");
+template <int D, bool LO> constexpr uint32_t smem_bytes() { return Map<D, LO>::OFF_CTL + (uint32_t)sizeof(Ctl) + 1024u; }
+static_assert(smem_bytes<128, true>() <= 227u * 1024u && smem_bytes<128, false>() <= 227u * 1024u, "shared memory");
+static_assert(smem_bytes<64, true>() > 114u * 1024u, "one block per SM: each allocates all of the TMEM");
 
 // mbar_wait with one answer for the whole warp: what follows a wait is done by all of its lanes or by none.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
@@ -265,11 +265,13 @@ struct alignas(64) Args {
   int n;
 };
 
-template <int D>
+// LO: K~ as two numbers per value.  Without: for calls that hand out no state, whose chains are whole (d = 128).
+template <int D, bool LO>
 __global__ void __launch_bounds__(kThreads, 1)
 decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log_decay, const int32_t* __restrict__ lens,
                 int64_t* __restrict__ pos, int* status, int H, int Tlen, int nseg, int early) {
-  using M = Map<D>;
+  using M = Map<D, LO>;
+  static_assert(LO || D == 128, "d = 64 takes hi and lo in one product");
   constexpr uint32_t SLOT = M::SLOT;
   constexpr int NSLOT = M::NSLOT, NX = D / 4;      // NX: values of X per thread of group C
   extern __shared__ unsigned char smem_dyn[];
@@ -320,7 +322,7 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
   const int tiles_all = bad ? 0 : (L + TILE - 1) / TILE, seg = (tiles_all + nseg - 1) / nseg * TILE;
   const int n0 = min(L, rank * seg), n1 = min(L, n0 + seg);
   const int nt = bad ? 0 : (n1 - n0 + TILE - 1) / TILE;
-  const int ns = nseg > 1 && rank < nseg - 1 ? nt : 0;             // tiles of the state pass
+  const int ns = LO && nseg > 1 && rank < nseg - 1 ? nt : 0;             // tiles of the state pass
   if (tid >= 96 && tid < 99) {
     const int n = (n1 - n0 + TILE - 1) % TILE + 1;
     ctl.fade[tid - 96] = decay_fade(bad ? 0.f : g, tid == 96 ? TILE : tid == 97 ? n : min(TILE, max(n1 - n0, 1)) - 1);
@@ -488,9 +490,9 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
           const uint32_t u = hi[4 * i + j];
           const float2 x = mul2(make_float2(lo_f(u), hi_f(u)), f);
           const uint32_t w = hi[4 * i + j] = pack2(x);
-          lo[j] = pack2(fma2(make_float2(lo_f(w), hi_f(w)), make_float2(-1.f, -1.f), x));
+          if (LO) lo[j] = pack2(fma2(make_float2(lo_f(w), hi_f(w)), make_float2(-1.f, -1.f), x));
         }
-        sts128(lp ^ (16u * i), lo[0], lo[1], lo[2], lo[3]);
+        if (LO) sts128(lp ^ (16u * i), lo[0], lo[1], lo[2], lo[3]);
       }
       return true;
     };
@@ -540,7 +542,7 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
       fence_async();
     };
 
-    if (nseg > 1) {                                // (a bad head's blocks pass through with zeros and write nothing)
+    if (LO && nseg > 1) {                          // (a bad head's blocks pass through with zeros and write nothing)
       // the sum of this block's segment, from nothing
       int left = rank < nseg - 1 ? n1 - n0 : 0;
       if (left > 0) ok = split_k(ring, min(TILE, left), M::OFF_LO) && put_k(ring, ring.next(), min(TILE, left));
@@ -579,7 +581,7 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
 #pragma unroll
       for (int i = 0; i < NX; ++i) X[i] = 0.f;
     }
-    if (nseg > 1) {
+    if (LO && nseg > 1) {
       if (rank > 0) {
         ok = __all_sync(0xffffffffu, mbar_wait_cluster(bar(B_SHARED), 0, abort)) && ok;
         for (int s = 0; ok && s < rank; ++s) {
@@ -621,7 +623,7 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
         mbar_arrive(bar(B_XRDY));
       }
     }
-    if (sw.S_out && !bad && rank == nseg - 1) {    // (the barrier inside is for every thread, whatever its waits said)
+    if (LO && sw.S_out && !bad && rank == nseg - 1) {    // (the barrier inside is for every thread, whatever its waits said)
       const Fade f = decay_fade(g, rev && L > 0 ? 1 : 0);
       if (D == 64) {                               // the two parts meet (lo is free: its last product has completed)
         if (!real)
@@ -659,13 +661,13 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
         const uint32_t v_lo = desc_lo(vt, BOX);
         if (D == 128) {
           product_mm(tmem + DX_COL, desc_lo(kt, BOX), v_lo, idesc(true, true, 128), false);
-          product_mm(tmem + DX_COL, desc_lo(lo, BOX), v_lo, idesc(true, true, 128), true);
+          if (LO) product_mm(tmem + DX_COL, desc_lo(lo, BOX), v_lo, idesc(true, true, 128), true);
         } else {                                   // hi and lo side by side: rows 0-63 and 64-127 of one product
           product_mm(tmem + DX_COL, desc_lo(kt, lo - kt), v_lo, idesc(true, true, 64), false);
         }
         mma_commit(bar(B_DXD));
       };
-      for (int t = 0; t < ns; ++t) {
+      for (int t = 0; LO && t < ns; ++t) {
         const Ring<NSLOT> rv = rk.next();
         ok = landed(rv) && k_made();
         if (ok && t > 0) ok = mbar_wait(bar(B_XRDY), x_at++ & 1, abort);       // the sum before has been read
@@ -834,8 +836,10 @@ cudaError_t launch_decay_tc(la_ctx* ctx, int B, int T, const DecayPasses& ps, co
   const int64_t chains = (int64_t)B * c.H * ps.n;
   const int nseg = segments(ctx, chains, (T + dtc::TILE - 1) / dtc::TILE);
   if (chains * nseg > INT32_MAX) return cudaErrorInvalidValue;
-  auto kern = c.d == 128 ? dtc::decay_tc_kernel<128> : dtc::decay_tc_kernel<64>;
-  const size_t smem = c.d == 128 ? dtc::smem_bytes<128>() : dtc::smem_bytes<64>();
+  bool state = nseg > 1 || c.d == 64 || ps.n == 1;   // (a forward call's outputs do not depend on whether it hands out its state)
+  for (int i = 0; i < ps.n; ++i) state = state || ps.p[i].S_out;
+  auto kern = c.d == 64 ? dtc::decay_tc_kernel<64, true> : state ? dtc::decay_tc_kernel<128, true> : dtc::decay_tc_kernel<128, false>;
+  const size_t smem = c.d == 64 ? dtc::smem_bytes<64, true>() : state ? dtc::smem_bytes<128, true>() : dtc::smem_bytes<128, false>();
   cudaError_t e = allow_smem((const void*)kern, ctx->device);
   if (e != cudaSuccess) return e;
   ctx->launches += 1;
