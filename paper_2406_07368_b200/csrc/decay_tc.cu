@@ -34,7 +34,7 @@ constexpr int kThreadsA = 256, kThreadsB = 128, kThreadsC = 512, kThreads = 1024
 constexpr int kWarpB = 8, kWarpC = 12, kMmaWarp = 28 /* its fellows 29 (loads), 30 (stores), 31 */;
 // Registers per thread once the roles have traded theirs: the launch gives everyone 64, per scheduler eight warps of them.
 // (No role may spill: nearly all of the SM's memory is shared memory, and a local load takes its way through the L2.)
-constexpr int kRegsA = 56, kRegsB = 64, kRegsC = 72, kRegsIssue = 48;
+constexpr int kRegsA = 48, kRegsB = 80, kRegsC = 72, kRegsIssue = 48;
 static_assert(2 * kRegsA + kRegsB + 4 * kRegsC + kRegsIssue == 8 * 64, "register split");
 constexpr uint32_t BOX = 128 * 128;                // 128 rows x 64 bf16, 128-byte swizzle
 constexpr uint32_t SC_COL = 0, O1_COL = 128, O2_COL = 256, DX_COL = 384, TMEM_COLS = 512;
@@ -400,6 +400,7 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
     }
   } else if (warp < kWarpC) {
     // =============================== group B: outputs ===============================
+    regs_up<kRegsB>();
     const int row = (warp - kWarpB) * 32 + lane, age = rev ? TILE - 1 - row : row;
     const uint32_t tl = tmem + ((uint32_t)((warp - kWarpB) * 32) << 16);
     __nv_bfloat16* o = (__nv_bfloat16*)sw.o.p + b * sw.o.sb + h * sw.o.sh;
@@ -414,19 +415,25 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
       const int n = count(t);
       __nv_bfloat16* to = o + (int64_t)(first(t) + row) * sw.o.st;
       const uint32_t at = sbase + ring.s * SLOT + r_at;
-#pragma unroll 1
+      // (the next 16 columns are on their way while these are packed: Q X of the next tile waits for the accumulators)
+      uint32_t x[2][16], y[2][16];
+      tmem_ld16(tl + O1_COL, x[0]);
+      tmem_ld16(tl + O2_COL, y[0]);
+#pragma unroll
       for (int c = 0; c < D / 16; ++c) {
-        uint32_t x[16], y[16], w[8];
-        tmem_ld16(tl + O1_COL + 16u * c, x);
-        tmem_ld16(tl + O2_COL + 16u * c, y);
+        uint32_t w[8];
         tmem_wait_ld();
-        if (c == D / 16 - 1) {
+        if (c + 1 < D / 16) {
+          tmem_ld16(tl + O1_COL + 16u * (c + 1), x[(c + 1) & 1]);
+          tmem_ld16(tl + O2_COL + 16u * (c + 1), y[(c + 1) & 1]);
+        } else {
           tc_before();
           mbar_arrive(bar(B_OF));
         }
+        const uint32_t(&xc)[16] = x[c & 1], (&yc)[16] = y[c & 1];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          w[i] = pack2(fma2(make_float2(f, f), make_float2(asf(y[2 * i]), asf(y[2 * i + 1])), make_float2(asf(x[2 * i]), asf(x[2 * i + 1]))));
+          w[i] = pack2(fma2(make_float2(f, f), make_float2(asf(yc[2 * i]), asf(yc[2 * i + 1])), make_float2(asf(xc[2 * i]), asf(xc[2 * i + 1]))));
         if (n == TILE) {
           const uint32_t p = (at ^ (32u * (c & 3))) + (D == 128 ? (uint32_t)(c >> 2) * BOX : 0u);
           sts128(p, w[0], w[1], w[2], w[3]);
@@ -687,17 +694,25 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
         tc_after();
         product_kk<D / 16>(tmem + SC_COL, q_lo, k_lo, idesc(false, false, 128));
         mma_commit(bar(B_QKD));
-        ok = k_made() && landed(rv);               // (K~ of this tile: the sum of the tile before has been read)
+        auto q_x = [&] {
+          if (!mbar_wait(bar(B_XRDY), x_at++ & 1, abort) || (t > 0 && !mbar_wait(bar(B_OF), (t - 1) & 1, abort))) return false;
+          tc_after();
+          product_km<D / 16>(tmem + O2_COL, q_lo, x_lo, idesc(false, true, D));
+          mma_commit(bar(B_QSD));
+          mma_commit(bar(B_EMPTY + rq.s));
+          return true;
+        };
+        auto k_v = [&] {                           // (K~ of this tile: the sum of the tile before has been read)
+          if (!k_made() || !landed(rv)) return false;
+          tc_after();
+          dx(sbase + rk.s * SLOT, sbase + rv.s * SLOT, here(lo_at));
+          mma_commit(bar(B_EMPTY + rk.s));
+          return true;
+        };
+        // The longer of the two last: with hi and lo that is K~^T V (first, one tile took 12.1 us and 16 of them 63.8, so
+        // 10.5 and 62.6), with hi alone Q X, which waits for the outputs before to have been read (gradients 148 us and 151).
+        ok = LO ? q_x() && k_v() : k_v() && q_x();
         if (!ok) break;
-        tc_after();
-        dx(sbase + rk.s * SLOT, sbase + rv.s * SLOT, here(lo_at));
-        mma_commit(bar(B_EMPTY + rk.s));
-        ok = mbar_wait(bar(B_XRDY), x_at++ & 1, abort) && (t == 0 || mbar_wait(bar(B_OF), (t - 1) & 1, abort));
-        if (!ok) break;
-        tc_after();
-        product_km<D / 16>(tmem + O2_COL, q_lo, x_lo, idesc(false, true, D));
-        mma_commit(bar(B_QSD));
-        mma_commit(bar(B_EMPTY + rq.s));
         ok = mbar_wait(bar(B_PRDY), t & 1, abort);
         if (!ok) break;
         tc_after();
