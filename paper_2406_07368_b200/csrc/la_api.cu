@@ -77,6 +77,7 @@ la_status decay_sweeps(la_ctx* ctx, int B, int T, const la::DecayPasses& ps, con
     const cudaError_t e = la::launch_decay_tc(ctx, B, T, ps, log_decay, lens, pos, s, &handled);
     if (e != cudaSuccess) return cuda_status(e);
     if (handled) return LA_OK;
+    return cuda_status(la::launch_decay_simt(ctx, B, T, ps, log_decay, lens, pos, s));
   }
   return cuda_status(la::launch_decay_walk(ctx, B, T, ps, log_decay, lens, pos, s));
 }

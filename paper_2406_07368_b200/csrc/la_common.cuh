@@ -205,6 +205,9 @@ struct DecayPasses {
 };
 cudaError_t launch_decay_walk(la_ctx* ctx, int B, int T, const DecayPasses& ps, const float* log_decay, const int32_t* lens,
                               int64_t* pos, cudaStream_t s);
+// ... chunkwise on the CUDA cores (fp32 io).
+cudaError_t launch_decay_simt(la_ctx* ctx, int B, int T, const DecayPasses& ps, const float* log_decay, const int32_t* lens,
+                              int64_t* pos, cudaStream_t s);
 // ... on the tensor cores (bf16 io).  Sets *handled to false when the type is not covered.
 cudaError_t launch_decay_tc(la_ctx* ctx, int B, int T, const DecayPasses& ps, const float* log_decay, const int32_t* lens,
                             int64_t* pos, cudaStream_t s, bool* handled);
