@@ -1,5 +1,5 @@
 // The recurrence with a decay in fp32 on the CUDA cores, chunkwise, for fp32 inputs: chunks of 64 tokens, every product an
-// fp32 multiply-add on register tiles fed by 128-bit shared-memory loads (eight loads for 64 multiply-adds).  Per chunk of n
+// fp32 multiply-add on register tiles fed by 128-bit shared-memory loads (twelve loads for 128 multiply-adds).  Per chunk of n
 // tokens, X the state before it (Fade: lam^n):
 //   P_ij = r upd lam^(i-j) q_i . k_j  (j <= i),   o_i = r lam^(i+1) q_i^T X + sum_j P_ij v_j
 //   k_j <- upd lam^(n-1-j) k_j,                   X <- lam^n X + sum_j k_j v_j^T
@@ -14,7 +14,8 @@ namespace la {
 namespace dsm {
 
 constexpr int C = 64, kMaxSeg = 8;
-template <int D> __host__ __device__ constexpr int threads() { return 4 * D; }
+constexpr int R = 8;                                 // rows of P and o per thread
+template <int D> __host__ __device__ constexpr int threads() { return C / R * (D / 4); }
 constexpr int PS = C + 4;                            // row stride of P; of q, k, v: D + 4 (eight rows in a row lie on different banks)
 template <int D> struct Smem {
   float q[C][D + 4], k[C][D + 4], v[C][D + 4], p[C][PS];
@@ -47,6 +48,7 @@ __global__ void __launch_bounds__(threads<D>(), D == 64 ? 2 : 1)
 decay_simt_kernel(const DecayPasses ps, const float* __restrict__ log_decay, const int32_t* __restrict__ lens,
                   int64_t* __restrict__ pos, int* status, int H, int Tlen, int nseg) {
   constexpr int NT = threads<D>(), TC = D / 4;       // threads; groups of 4 columns
+  constexpr int S = C / R;                           // groups of rows; a thread's rows lie S apart
   constexpr int UJ = C / TC;                         // P: columns tc + TC u of a thread
   constexpr int XR = D * D / NT / 4;                 // rows of X per thread (4 columns each)
   extern __shared__ unsigned char smem_raw[];
@@ -71,8 +73,8 @@ decay_simt_kernel(const DecayPasses ps, const float* __restrict__ log_decay, con
   if (tid <= C) sm.pw[tid] = bad ? 0.f : decay_pow(g, tid);
   const Fade fade_c = decay_fade(bad ? 0.f : g, C);
 
-  // A thread's place: 4 x 8 of them in a warp, so that either operand of a tile is one wavefront of shared memory per load.
-  // X: rows XR ti ..., columns 4 tc ...;  o: rows ti + 16 u, columns 4 tc ...;  P: rows ti + 16 u, columns tc + TC u.
+  // A thread's place: 4 x 8 of them in a warp.
+  // X: rows XR ti ..., columns 4 tc ...;  o: rows ti + C / R u, columns 4 tc ...;  P: rows ti + C / R u, columns tc + TC u.
   const int w = tid / 32, ti = w / (TC / 8) * 4 + tid % 32 / 8, tc = w % (TC / 8) * 8 + tid % 8;
   float2 X[XR][2];
 #pragma unroll
@@ -175,81 +177,80 @@ decay_simt_kernel(const DecayPasses ps, const float* __restrict__ log_decay, con
     load(k, p.k.st, sm.k, at, n);
     load(v, p.v.st, sm.v, at, n);
     landed();
-    // ---- P; blocks of 16 rows and TC columns that lie behind the diagonal are not formed ----
+    // ---- P; blocks of 8 rows and TC columns that lie behind the diagonal are not formed ----
     {
-      float2 acc[4][UJ];                             // (even and odd features)
+      float acc[R][UJ];
 #pragma unroll
-      for (int a = 0; a < 4; ++a)
+      for (int a = 0; a < R; ++a)
 #pragma unroll
-        for (int c = 0; c < UJ; ++c) acc[a][c] = make_float2(0.f, 0.f);
-#pragma unroll 4
+        for (int c = 0; c < UJ; ++c) acc[a][c] = 0.f;
+#pragma unroll 2
       for (int d = 0; d < D; d += 4) {
-        float qa[4][4], kc[UJ][4];
+        float qa[R][4], kc[UJ][4];
 #pragma unroll
-        for (int a = 0; a < 4; ++a) get4(&sm.q[ti + 16 * a][d], qa[a]);
+        for (int a = 0; a < R; ++a) get4(&sm.q[ti + S * a][d], qa[a]);
 #pragma unroll
         for (int c = 0; c < UJ; ++c) get4(&sm.k[tc + TC * c][d], kc[c]);
 #pragma unroll
-        for (int a = 0; a < 4; ++a)
+        for (int x = 0; x < 4; ++x)
 #pragma unroll
-          for (int c = 0; c < UJ; ++c)
-            if (TC * c < 16 * a + 16)
+          for (int a = 0; a < R; ++a)
 #pragma unroll
-              for (int x = 0; x < 4; x += 2)
-                acc[a][c] = __ffma2_rn(make_float2(qa[a][x], qa[a][x + 1]), make_float2(kc[c][x], kc[c][x + 1]), acc[a][c]);
+            for (int c = 0; c < UJ; ++c)
+              if (TC * c < S * a + S) acc[a][c] = fmaf(qa[a][x], kc[c][x], acc[a][c]);
       }
 #pragma unroll
-      for (int a = 0; a < 4; ++a)
+      for (int a = 0; a < R; ++a)
 #pragma unroll
         for (int c = 0; c < UJ; ++c) {
-          const int i = ti + 16 * a, j = tc + TC * c;
-          if (TC * c < 16 * a + 16) sm.p[i][j] = j <= i ? (acc[a][c].x + acc[a][c].y) * (p.r * p.upd * sm.pw[i - j]) : 0.f;
+          const int i = ti + S * a, j = tc + TC * c;
+          if (TC * c < S * a + S) sm.p[i][j] = j <= i ? acc[a][c] * (p.r * p.upd * sm.pw[i - j]) : 0.f;
         }
     }
     __syncthreads();
     // ---- outputs: r lam^(i+1) Q X, then P V up to the diagonal ----
     {
-      float2 acc[4][2];
+      float2 acc[R][2];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) acc[u][0] = acc[u][1] = make_float2(0.f, 0.f);
-#pragma unroll 4
+      for (int u = 0; u < R; ++u) acc[u][0] = acc[u][1] = make_float2(0.f, 0.f);
+#pragma unroll 2
       for (int a = 0; a < D; a += 4) {
-        float qi[4][4], x[4][4];
+        float qi[R][4], x[4][4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) get4(&sm.q[ti + 16 * u][a], qi[u]);
+        for (int u = 0; u < R; ++u) get4(&sm.q[ti + S * u][a], qi[u]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) get4(&sm.X[a + j][4 * tc], x[j]);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int u = 0; u < 4; ++u) add4(acc[u], qi[u][j], x[j]);
+          for (int u = 0; u < R; ++u) add4(acc[u], qi[u][j], x[j]);
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float f = p.r * sm.pw[ti + 16 * u + 1 - e];
+      for (int u = 0; u < R; ++u) {
+        const float f = p.r * sm.pw[ti + S * u + 1 - e];
 #pragma unroll
         for (int c = 0; c < 2; ++c) acc[u][c] = make_float2(acc[u][c].x * f, acc[u][c].y * f);
       }
-      // 16 tokens at a time: rows of the same 16 as far as the diagonal, the rows behind them all
+      // 8 tokens at a time: rows of the same 8 as far as the diagonal, the rows behind them all
 #pragma unroll
-      for (int b16 = 0; b16 < 4; ++b16)
-#pragma unroll 2
-        for (int j0 = 0; j0 < 16; j0 += 4) {
-          float pu[4][4], x[4][4];
+      for (int s = 0; s < R; ++s)
 #pragma unroll
-          for (int u = b16; u < 4; ++u) get4(&sm.p[ti + 16 * u][16 * b16 + j0], pu[u]);
+        for (int j0 = 0; j0 < S; j0 += 4) {
+          float pu[R][4], x[4][4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) get4(&sm.v[16 * b16 + j0 + j][4 * tc], x[j]);
+          for (int u = s; u < R; ++u) get4(&sm.p[ti + S * u][S * s + j0], pu[u]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) get4(&sm.v[S * s + j0 + j][4 * tc], x[j]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            if (j0 + j <= ti) add4(acc[b16], pu[b16][j], x[j]);
+            if (j0 + j <= ti) add4(acc[s], pu[s][j], x[j]);
 #pragma unroll
-            for (int u = b16 + 1; u < 4; ++u) add4(acc[u], pu[u][j], x[j]);
+            for (int u = s + 1; u < R; ++u) add4(acc[u], pu[u][j], x[j]);
           }
         }
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (ti + 16 * u < n) *reinterpret_cast<float4*>(o + row(at + ti + 16 * u) * p.o.st + 4 * tc) = make_float4(acc[u][0].x, acc[u][0].y, acc[u][1].x, acc[u][1].y);
+      for (int u = 0; u < R; ++u)
+        if (ti + S * u < n) *reinterpret_cast<float4*>(o + row(at + ti + S * u) * p.o.st + 4 * tc) = make_float4(acc[u][0].x, acc[u][0].y, acc[u][1].x, acc[u][1].y);
     }
     scale_k(n);                                      // (P has been formed: K as it was is not wanted any more)
     __syncthreads();
@@ -275,8 +276,7 @@ cudaError_t launch_decay_simt(la_ctx* ctx, int B, int T, const DecayPasses& ps, 
   const la_config& c = ctx->cfg;
   const int64_t chains = (int64_t)B * c.H * ps.n;
   const int chunks = (T + dsm::C - 1) / dsm::C, places = ctx->sm_count * (c.d == 64 ? 2 : 1);
-  // As many segments as there are places for all chains' (a segment's sum costs a third of its outputs: two gain nothing),
-  // evenly long.
+  // (a segment's sum costs a third of its outputs)
   int nseg = 1;
   while (nseg < dsm::kMaxSeg && chains * nseg * 2 <= places && chunks >= nseg * 2) nseg *= 2;
   if (chains * nseg > INT32_MAX) return cudaErrorInvalidValue;
@@ -285,7 +285,7 @@ cudaError_t launch_decay_simt(la_ctx* ctx, int B, int T, const DecayPasses& ps, 
   const cudaError_t e = allow_smem((const void*)kern, ctx->device);
   if (e != cudaSuccess) return e;
   ctx->launches += 1;
-  return launch_cluster(nseg, true, kern, dim3((unsigned)(chains * nseg)), dim3(c.d * 4), smem, s, ps, log_decay, lens, pos,
+  return launch_cluster(nseg, true, kern, dim3((unsigned)(chains * nseg)), dim3(c.d == 64 ? dsm::threads<64>() : dsm::threads<128>()), smem, s, ps, log_decay, lens, pos,
                         ctx->d_status, c.H, T, nseg);
 }
 
