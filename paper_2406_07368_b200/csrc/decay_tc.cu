@@ -457,7 +457,6 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
     const int krow = ct & 127, kage = rev ? TILE - 1 - krow : krow, kh = ct >> 7;        // a row and a quarter of a tile
     const uint32_t tx = tmem + DX_COL + ((uint32_t)(q4 * 32) << 16) + (uint32_t)(hf * NX);
     const bool real = D == 128 || q4 < 2;          // d = 64: rows 64 ... hold the part of X that comes from lo
-    auto sat = [&] { return ((size_t)here(bh) * D + here(a)) * D + here(hf) * NX; };   // (rarely wanted: not kept)
     // Quarter i of a row: four pieces from piece 4 (i & 1) on of box i >> 1, or (d = 64) two pieces from 2 i on.
     auto quarter = [&](int row, int i) {
       return D == 128 ? (uint32_t)(i >> 1) * BOX + (row_at(row) ^ (64u * (i & 1))) : row_at(row) ^ (32u * i);
@@ -549,6 +548,15 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
       fence_async();
     };
 
+    // X by rows in the memory of LO and of the bf16 copy (128 rows of D floats, 16-byte pieces swizzled by row), for the way
+    // to and from a state in HBM: a thread's own part of it is 16 bytes in each of 32 rows per access of a warp, which took
+    // 3 us for one state.
+    auto piece = [&](int r, int i) { return reinterpret_cast<float4*>(smem + M::OFF_LO + (uint32_t)r * (D * 4) + (uint32_t)((i ^ (r & 7)) << 4)); };
+    auto rows_at = [&](int r, int i) { return *piece(r, i); };
+    auto put_rows = [&] {
+#pragma unroll
+      for (int i = 0; i < NX / 4; ++i) *piece(a, hf * (NX / 4) + i) = make_float4(X[4 * i], X[4 * i + 1], X[4 * i + 2], X[4 * i + 3]);
+    };
     if (LO && nseg > 1) {                          // (a bad head's blocks pass through with zeros and write nothing)
       // the sum of this block's segment, from nothing
       int left = rank < nseg - 1 ? n1 - n0 : 0;
@@ -572,21 +580,30 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
       }
     }
     // X before the segment: the caller's state, then the sums of the segments before this one
-    if (sw.S_in && real && !bad) {
+#pragma unroll
+    for (int i = 0; i < NX; ++i) X[i] = 0.f;
+    if (sw.S_in && !bad) {
       if (sw.trans) {
         const float* p = sw.S_in + ((size_t)here(bh) * D + here(hf) * NX) * D + a;
+        if (real)
 #pragma unroll
-        for (int i = 0; i < NX; ++i) X[i] = p[(size_t)i * D];
+          for (int i = 0; i < NX; ++i) X[i] = p[(size_t)i * D];
       } else {
-#pragma unroll
-        for (int i = 0; i < NX; i += 4) {
-          const float4 v = *reinterpret_cast<const float4*>(sw.S_in + sat() + i);
-          X[i] = v.x, X[i + 1] = v.y, X[i + 2] = v.z, X[i + 3] = v.w;
+        const float4* p = reinterpret_cast<const float4*>(sw.S_in + (size_t)here(bh) * D * D);
+        if (LO && nseg == 1) {
+          for (int i = ct; i < D * D / 4; i += kThreadsC) *piece(i / (D / 4), i % (D / 4)) = p[i];
+          sync_c();
+          p = nullptr;
         }
-      }
-    } else {
+        if (real)
 #pragma unroll
-      for (int i = 0; i < NX; ++i) X[i] = 0.f;
+          for (int i = 0; i < NX / 4; ++i) {
+            const int at = hf * (NX / 4) + i;
+            const float4 v = p ? p[a * (D / 4) + at] : rows_at(a, at);
+            X[4 * i] = v.x, X[4 * i + 1] = v.y, X[4 * i + 2] = v.z, X[4 * i + 3] = v.w;
+          }
+        if (LO && nseg == 1) sync_c();             // (the copy and lo go there next)
+      }
     }
     if (LO && nseg > 1) {
       if (rank > 0) {
@@ -631,25 +648,18 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
       }
     }
     if (LO && sw.S_out && !bad && rank == nseg - 1) {    // (the barrier inside is for every thread, whatever its waits said)
+      put_rows();
+      sync_c();
       const Fade f = decay_fade(g, rev && L > 0 ? 1 : 0);
-      if (D == 64) {                               // the two parts meet (lo is free: its last product has completed)
-        if (!real)
-#pragma unroll
-          for (int i = 0; i < NX / 4; ++i)
-            *reinterpret_cast<float4*>(smem + M::OFF_LO + (uint32_t)((i * 4 + hf) * 64 + a - 64) * 16u) =
-                make_float4(X[4 * i], X[4 * i + 1], X[4 * i + 2], X[4 * i + 3]);
-        sync_c();
-        if (real)
-#pragma unroll
-          for (int i = 0; i < NX / 4; ++i) {
-            const float4 v = *reinterpret_cast<const float4*>(smem + M::OFF_LO + (uint32_t)((i * 4 + hf) * 64 + a) * 16u);
-            X[4 * i] += v.x, X[4 * i + 1] += v.y, X[4 * i + 2] += v.z, X[4 * i + 3] += v.w;
-          }
+      constexpr int PR = D / 4;                    // pieces of a row
+      for (int i = ct; ok && i < D * PR; i += kThreadsC) {
+        float4 v = rows_at(i / PR, i % PR);
+        if (D == 64) {                             // the parts that came from hi and from lo
+          const float4 u = rows_at(i / PR + 64, i % PR);
+          v = make_float4(v.x + u.x, v.y + u.y, v.z + u.z, v.w + u.w);
+        }
+        *reinterpret_cast<float4*>(sw.S_out + (size_t)bh * D * D + (size_t)i * 4) = make_float4(f(v.x), f(v.y), f(v.z), f(v.w));
       }
-      if (real && ok)
-#pragma unroll
-        for (int i = 0; i < NX; i += 4)
-          *reinterpret_cast<float4*>(sw.S_out + sat() + i) = make_float4(f(X[i]), f(X[i + 1]), f(X[i + 2]), f(X[i + 3]));
     }
   } else {
     regs_down<kRegsIssue>();

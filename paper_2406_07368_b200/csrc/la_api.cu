@@ -69,10 +69,20 @@ bool norm_rope_args_ok(const la_ctx* ctx, const la_norm_rope_args* a) {
   if (!a || a->rot < 0 || a->rot > ctx->cfg.d || a->rot % 16 || (a->rot && !a->inv_freq) || !std::isfinite(a->mscale)) return false;
   return !a->norm || (std::isfinite(a->eps) && a->eps >= 0.f && aligned16(a->wq) && aligned16(a->wk));
 }
+// Whether walking the tokens (decay_walk.cu) is faster than going through them by chunks: a chunk costs the same however few
+// tokens it holds, a token its time in every one of D / 32 blocks per chain.  The tokens up to which it is, measured inside
+// graphs for 4 to 2048 chains a sweep: bf16 (us, walk / tensor cores, 512 chains, d = 64: 24 tokens 18 / 25, 48: 31 / 25;
+// d = 128: 8: 23 / 34, 16: 37 / 34), fp32 (512 chains, d = 128: 32 tokens 70 / 88, 48: 103 / 91).  With chains for half the SMs
+// or fewer a walk has the GPU to itself and a chunk is latency (32 chains, d = 128: bf16 24 tokens 7.3 / 8.0; fp32 128: 30 / 33).
+bool decay_walks(const la_ctx* ctx, int64_t chains, int T) {
+  const bool few = 2 * chains <= ctx->sm_count, narrow = ctx->cfg.d == 64;
+  if (ctx->cfg.io_dtype == LA_BF16) return T <= (narrow ? 28 : few ? 24 : 11);
+  return T <= (!few ? 38 : narrow ? 52 : 160);
+}
 // The sweeps of one call of the layer with a decay.
 la_status decay_sweeps(la_ctx* ctx, int B, int T, const la::DecayPasses& ps, const float* log_decay, const int32_t* lens,
                        int64_t* pos, cudaStream_t s) {
-  if (ctx->prefill_kernel == 0 && T > 16) {
+  if (ctx->prefill_kernel == 0 && !decay_walks(ctx, (int64_t)B * ctx->cfg.H * ps.n, T)) {
     bool handled = false;
     const cudaError_t e = la::launch_decay_tc(ctx, B, T, ps, log_decay, lens, pos, s, &handled);
     if (e != cudaSuccess) return cuda_status(e);
