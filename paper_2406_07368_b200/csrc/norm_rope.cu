@@ -1,12 +1,15 @@
 // Norms of the queries and keys of each head and the rotation by their positions, in one pass over both, and the
 // gradients.  Bound by HBM: every row is read once and written once.
 //
-// A row of d values is held by d / 8 lanes, eight values each (one or two 128-bit loads), so that a warp works on two or
-// four rows at a time and the mean over a row is a sum over 16 or 8 lanes.  A work item is a token and some of its 2 H
-// rows (the q heads, then the k heads): the angles of a token are the same for all of them.  They are formed once per
-// item, d / 2 of them spread over the warp's lanes, and passed on through shared memory:
+// A row of d values is held by d / 8 lanes, four values each in two places, so that both values of a rotated pair are in
+// one lane: m ... m + 3 and rot / 2 + m ... (pairs half a rotation apart), or eight in a row (neighbours are pairs).  Rows
+// are read in batches, all loads of a batch in flight together.  A warp works on two or four rows at a time, and the mean
+// over a row is a sum over 16 or 8 lanes.  A work item is a token and some of its 2 H rows (the q heads, then the k heads):
+// the angles of a token, four per lane, are the same for all of them and stay in registers.
 //   turns = p (f / 2 pi) in 64 bits, minus its nearest integer; only that remainder, at most half a turn, goes to fp32
 // (in 32 bits a position of 10^6 alone would leave an angle of the first pair wrong by 0.06).
+// (With eight values in a row per lane whatever the pairs, partners fetched by shuffles and cos, sin and the weights read from
+// shared memory row by row: 4 x 2048 tokens, 32 heads, d = 128: 93 us, gradients 156, 85 % of the L1's throughput.)
 #include "decay.cuh"
 
 namespace la {
@@ -22,106 +25,164 @@ struct Args {
   int norm, rot, interleaved;
 };
 
-// cos and sin (times mscale) of the item's token, pair m at cs[m].
-__device__ __forceinline__ void angles(const Args& a, int b, int t, int lane, float2* cs) {
-  const double p = (double)((a.pos ? a.pos[b] : 0) + t);
-  __syncwarp();                                    // (the item before has read its angles)
-  for (int m = lane; m < a.rot / 2; m += 32) {
-    const double turns = p * (a.inv_freq[m] * 0.15915494309189533577);
-    float s, c;
-    sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
-    cs[m] = make_float2(c * a.mscale, s * a.mscale);
-  }
-  __syncwarp();
-}
+// (Two fp32 numbers per instruction; each half rounds as the scalar one does.)
+__device__ __forceinline__ float2 f2(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 mul(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
 
-// Rotates the row whose values 8 l ... 8 l + 7 are in lane l of a group of LPR lanes; sgn = -1: by minus the angle.
-template <int LPR>
-__device__ __forceinline__ void rotate(const Args& a, const float2* cs, int l, float sgn, float (&x)[8]) {
-  const int first = 8 * l;
-  if (a.interleaved) {
-    if (first < a.rot) {
+// Four values of the io type, as they lie in memory and as fp32.
+template <typename T> struct Raw4;
+template <> struct Raw4<float> {
+  float4 v;
+  __device__ __forceinline__ void load(const float* p) { v = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ void zero() { v = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void get(float2* x) const { x[0] = make_float2(v.x, v.y), x[1] = make_float2(v.z, v.w); }
+  static __device__ __forceinline__ void store(float* p, const float2* x) { *reinterpret_cast<float4*>(p) = make_float4(x[0].x, x[0].y, x[1].x, x[1].y); }
+};
+template <> struct Raw4<__nv_bfloat16> {
+  uint2 v;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void zero() { v = make_uint2(0u, 0u); }
+  __device__ __forceinline__ void get(float2* x) const {
+    x[0] = make_float2(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u));
+    x[1] = make_float2(__uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
+  }
+  static __device__ __forceinline__ void store(__nv_bfloat16* p, const float2* x) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(x[0].x, x[0].y), b = __floats2bfloat162_rn(x[1].x, x[1].y);
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+  }
+};
+
+// A lane's place in a row: values lo ... lo + 3 and hi ... hi + 3; turned: they are four pairs that rotate.
+struct Lane {
+  int lo, hi;
+  bool turned;
+  template <bool INTER> static __device__ __forceinline__ Lane at(int l, int rot) {
+    if (INTER) return {8 * l, 8 * l + 4, 8 * l < rot};
+    return 8 * l < rot ? Lane{4 * l, rot / 2 + 4 * l, true} : Lane{8 * l, 8 * l + 4, false};
+  }
+};
+// A lane's eight values; neighbours in one access where the type makes that 16 bytes.
+template <bool INTER, typename T> __device__ __forceinline__ void load8(const T* row, const Lane& at, Raw4<T>& a, Raw4<T>& b) {
+  if constexpr (INTER && sizeof(T) == 2) {
+    const uint4 u = *reinterpret_cast<const uint4*>(row + at.lo);
+    a.v = make_uint2(u.x, u.y), b.v = make_uint2(u.z, u.w);
+  } else {
+    a.load(row + at.lo), b.load(row + at.hi);
+  }
+}
+template <bool INTER, typename T> __device__ __forceinline__ void store8(T* row, const Lane& at, const float2 (&x)[4]) {
+  if constexpr (INTER && sizeof(T) == 2) {
+    uint32_t w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 c = cs[first / 2 + i];
-        const float s = sgn * c.y, u = x[2 * i], w = x[2 * i + 1];
-        x[2 * i] = fmaf(u, c.x, -w * s);
-        x[2 * i + 1] = fmaf(w, c.x, u * s);
-      }
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(x[i].x, x[i].y);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
-    return;
-  }
-  const int half = a.rot / 16;                     // lanes of half the rotated values
-  const int other = l < half ? l + half : l < 2 * half ? l - half : l;
-  float y[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(0xffffffffu, x[i], other, LPR);
-  if (l < 2 * half) {
-    const float2* c = cs + 8 * (l < half ? l : other);
-    const float sg = l < half ? -sgn : sgn;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = fmaf(x[i], c[i].x, y[i] * (sg * c[i].y));
+    *reinterpret_cast<uint4*>(row + at.lo) = make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+    Raw4<T>::store(row + at.lo, x), Raw4<T>::store(row + at.hi, x + 2);
   }
 }
-
+// cos and sin (times mscale) of the lane's four pairs; a lane without any gets 1 and 0.  The lanes that hold the same place
+// of different rows share out the work.
+template <int RPW> __device__ __forceinline__ void angles(const Args& a, int b, int t, int l, int r0, float2 (&cs)[4]) {
+  const double p = (double)((a.pos ? a.pos[b] : 0) + t);
+  constexpr int EACH = 4 / RPW, LPR = 32 / RPW;
+  float2 mine[EACH];
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const int m = 4 * l + r0 * EACH + i;
+    float s = 0.f, c = 1.f;
+    if (2 * m < a.rot) {
+      const double turns = p * (a.inv_freq[m] * 0.15915494309189533577);
+      sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
+      s *= a.mscale, c *= a.mscale;
+    }
+    mine[i] = make_float2(c, s);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    cs[i] = make_float2(__shfl_sync(0xffffffffu, mine[i % EACH].x, i / EACH * LPR + l), __shfl_sync(0xffffffffu, mine[i % EACH].y, i / EACH * LPR + l));
+}
+// Rotates the four pairs of x (lo in x[0], x[1], hi in x[2], x[3]); sgn = -1: by minus the angle.
+template <bool INTER> __device__ __forceinline__ void rotate(const float2 (&cs)[4], float sgn, float2 (&x)[4]) {
+  if (INTER) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float s = sgn * cs[i].y;
+      x[i] = fma(x[i], f2(cs[i].x), mul(make_float2(x[i].y, x[i].x), make_float2(-s, s)));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float2 c = make_float2(cs[2 * i].x, cs[2 * i + 1].x), s = mul(f2(sgn), make_float2(cs[2 * i].y, cs[2 * i + 1].y)), u = x[i], w = x[i + 2];
+      x[i] = fma(u, c, mul(w, mul(f2(-1.f), s)));
+      x[i + 2] = fma(w, c, mul(u, s));
+    }
+  }
+}
 template <int LPR> __device__ __forceinline__ float row_sum(float x) {
 #pragma unroll
   for (int o = LPR / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o, LPR);
   return x;
 }
-__device__ __forceinline__ int64_t at(const la_view& v, int b, int h, int t) { return b * v.sb + h * v.sh + t * v.st; }
-__device__ __forceinline__ void weights(const float* w, int l, float (&x)[8]) {
-  if (w) {
-    Io8<float>::load(w + 8 * l, x);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = 1.f;
-  }
+__device__ __forceinline__ void weights(const float* w, const Lane& at, float2 (&x)[4]) {
+  if (w) Raw4<float>{*reinterpret_cast<const float4*>(w + at.lo)}.get(x), Raw4<float>{*reinterpret_cast<const float4*>(w + at.hi)}.get(x + 2);
+  else x[0] = x[1] = x[2] = x[3] = f2(1.f);
+}
+__device__ __forceinline__ float squares(const float2 (&x)[4]) {
+  const float2 s = fma(x[0], x[0], fma(x[1], x[1], fma(x[2], x[2], mul(x[3], x[3]))));
+  return s.x + s.y;
 }
 
 // parts: a token's rows are shared out over this many items
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads)
+template <typename T, int D, bool INTER>
+__global__ void __launch_bounds__(kThreads, 4)
 norm_rope_kernel(const Args a, const la_view q, const la_view k, const la_view qo, const la_view ko, int H, int Tlen,
                  int64_t items, int parts) {
-  constexpr int LPR = D / 8, RPW = 32 / LPR;       // lanes per row, rows per warp
-  __shared__ float2 cs_all[kWarps][D / 2];
+  constexpr int LPR = D / 8, RPW = 32 / LPR, BATCH = sizeof(T) == 2 ? 4 : 2;   // lanes per row, rows per warp, of them in flight
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % LPR, r0 = lane / LPR;
-  float2* cs = cs_all[warp];
+  const Lane at = Lane::at<INTER>(l, a.rot);
   pdl_wait();
   pdl_trigger();
   const int per = (2 * H + parts - 1) / parts;
   for (int64_t it = (int64_t)blockIdx.x * kWarps + warp; it < items; it += (int64_t)gridDim.x * kWarps) {
     const int64_t tok = it / parts;
     const int b = (int)(tok / Tlen), t = (int)(tok % Tlen), lo = (int)(it % parts) * per, hi = min(2 * H, lo + per);
-    angles(a, b, t, lane, cs);
-    for (int base = lo; base < hi; base += RPW) {
-      const int row = base + r0;
-      const bool live = row < hi, isk = row >= H;
-      const int h = isk ? row - H : row;
-      float x[8], w[8];
-      if (live) {
-        const la_view& v = isk ? k : q;
-        Io8<T>::load((const T*)v.p + at(v, b, h, t) + 8 * l, x);
-      } else {
+    float2 cs[4];
+    angles<RPW>(a, b, t, l, r0, cs);
+    auto rows = [&](const la_view& in, const la_view& out, const float* wp, int h0, int h1) {
+      float2 w[4];
+      weights(a.norm ? wp : nullptr, at, w);
+      const T* src = (const T*)in.p + b * in.sb + t * in.st;
+      T* dst = (T*)out.p + b * out.sb + t * out.st;
+      for (int base = h0; base < h1; base += RPW * BATCH) {
+        Raw4<T> x0[BATCH], x1[BATCH];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = 0.f;
-      }
-      if (a.norm) {
-        float s = 0.f;
+        for (int i = 0; i < BATCH; ++i) {
+          const int h = base + i * RPW + r0;
+          if (h < h1) load8<INTER>(src + h * in.sh, at, x0[i], x1[i]);
+          else x0[i].zero(), x1[i].zero();
+        }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
-        const float rs = 1.f / sqrtf(row_sum<LPR>(s) * (1.f / D) + a.eps);
-        weights(isk ? a.wk : a.wq, l, w);
+        for (int i = 0; i < BATCH; ++i) {
+          if (base + i * RPW >= h1) break;         // (the same for the whole warp)
+          const int h = base + i * RPW + r0;
+          float2 x[4];
+          x0[i].get(x), x1[i].get(x + 2);
+          if (a.norm) {
+            const float rs = rsqrtf(row_sum<LPR>(squares(x)) * (1.f / D) + a.eps);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] *= rs * w[i];
+            for (int j = 0; j < 4; ++j) x[j] = mul(x[j], mul(f2(rs), w[j]));
+          }
+          if (at.turned) rotate<INTER>(cs, 1.f, x);
+          if (h < h1) store8<INTER>(dst + h * out.sh, at, x);
+        }
       }
-      rotate<LPR>(a, cs, l, 1.f, x);
-      if (live) {
-        const la_view& v = isk ? ko : qo;
-        Io8<T>::store((T*)v.p + at(v, b, h, t) + 8 * l, x);
-      }
-    }
+    };
+    rows(q, qo, a.wq, min(lo, H), min(hi, H));
+    rows(k, ko, a.wk, max(lo, H) - H, max(hi, H) - H);
   }
 }
 
@@ -129,74 +190,80 @@ norm_rope_kernel(const Args a, const la_view q, const la_view k, const la_view q
 //   dw += u xh,   dx = rs (w u - xh mean(w u xh)).
 // Each warp keeps its part of dw in registers, the q rows and the k rows apart; a block adds up its warps' parts and
 // writes them to its place in `part`.
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads)
+template <typename T, int D, bool INTER>
+__global__ void __launch_bounds__(kThreads, 2)
 norm_rope_backward_kernel(const Args a, const la_view q, const la_view k, const la_view gq, const la_view gk, const la_view dq,
                           const la_view dk, float* __restrict__ part, int H, int Tlen, int64_t items, int parts) {
-  constexpr int LPR = D / 8, RPW = 32 / LPR;
-  __shared__ float2 cs_all[kWarps][D / 2];
+  constexpr int LPR = D / 8, RPW = 32 / LPR, BATCH = sizeof(T) == 2 ? 4 : 2;
   __shared__ float sums[kWarps][2][D];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % LPR, r0 = lane / LPR;
-  float2* cs = cs_all[warp];
+  const Lane at = Lane::at<INTER>(l, a.rot);
   pdl_wait();
   pdl_trigger();
-  float dw[2][8];
+  float2 dw[2][4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) dw[0][i] = dw[1][i] = 0.f;
+  for (int i = 0; i < 4; ++i) dw[0][i] = dw[1][i] = f2(0.f);
   const int per = (2 * H + parts - 1) / parts;
   for (int64_t it = (int64_t)blockIdx.x * kWarps + warp; it < items; it += (int64_t)gridDim.x * kWarps) {
     const int64_t tok = it / parts;
     const int b = (int)(tok / Tlen), t = (int)(tok % Tlen), lo = (int)(it % parts) * per, hi = min(2 * H, lo + per);
-    angles(a, b, t, lane, cs);
-    for (int base = lo; base < hi; base += RPW) {
-      const int row = base + r0;
-      const bool live = row < hi, isk = row >= H;
-      const int h = isk ? row - H : row;
-      float x[8], u[8], w[8];
-      if (live) {
-        const la_view &v = isk ? k : q, &gv = isk ? gk : gq;
-        Io8<T>::load((const T*)v.p + at(v, b, h, t) + 8 * l, x);
-        Io8<T>::load((const T*)gv.p + at(gv, b, h, t) + 8 * l, u);
-      } else {
+    float2 cs[4];
+    angles<RPW>(a, b, t, l, r0, cs);
+    auto rows = [&](const la_view& in, const la_view& gin, const la_view& out, const float* wp, float2 (&sum)[4], int h0, int h1) {
+      float2 w[4];
+      weights(a.norm ? wp : nullptr, at, w);
+      const T* src = (const T*)in.p + b * in.sb + t * in.st;
+      const T* gsrc = (const T*)gin.p + b * gin.sb + t * gin.st;
+      T* dst = (T*)out.p + b * out.sb + t * out.st;
+      for (int base = h0; base < h1; base += RPW * BATCH) {
+        Raw4<T> x0[BATCH], x1[BATCH], g0[BATCH], g1[BATCH];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = u[i] = 0.f;
-      }
-      rotate<LPR>(a, cs, l, -1.f, u);
-      if (a.norm) {
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
-        s = row_sum<LPR>(s);
-        const float rs = live ? 1.f / sqrtf(s * (1.f / D) + a.eps) : 0.f;
-        weights(isk ? a.wk : a.wq, l, w);
-        float m = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          x[i] *= rs;
-          const float d = u[i] * x[i];
-          if (isk) dw[1][i] += d;
-          else dw[0][i] += d;
-          m = fmaf(w[i], d, m);
+        for (int i = 0; i < BATCH; ++i) {
+          const int h = base + i * RPW + r0;
+          if (h < h1) {
+            load8<INTER>(src + h * in.sh, at, x0[i], x1[i]);
+            load8<INTER>(gsrc + h * gin.sh, at, g0[i], g1[i]);
+          } else {
+            x0[i].zero(), x1[i].zero(), g0[i].zero(), g1[i].zero();
+          }
         }
-        m = row_sum<LPR>(m) * (1.f / D);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) u[i] = rs * fmaf(w[i], u[i], -x[i] * m);
+        for (int i = 0; i < BATCH; ++i) {
+          if (base + i * RPW >= h1) break;
+          const int h = base + i * RPW + r0;
+          float2 x[4], u[4];
+          x0[i].get(x), x1[i].get(x + 2), g0[i].get(u), g1[i].get(u + 2);
+          if (at.turned) rotate<INTER>(cs, -1.f, u);
+          if (a.norm) {
+            const float s = row_sum<LPR>(squares(x)), rs = h < h1 ? rsqrtf(s * (1.f / D) + a.eps) : 0.f;
+            float2 m2 = f2(0.f);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              x[j] = mul(x[j], f2(rs));
+              const float2 d = mul(u[j], x[j]);
+              sum[j] = __fadd2_rn(sum[j], d);
+              m2 = fma(w[j], d, m2);
+            }
+            const float m = row_sum<LPR>(m2.x + m2.y) * (-1.f / D);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[j] = mul(f2(rs), fma(w[j], u[j], mul(x[j], f2(m))));
+          }
+          if (h < h1) store8<INTER>(dst + h * out.sh, at, u);
+        }
       }
-      if (live) {
-        const la_view& v = isk ? dk : dq;
-        Io8<T>::store((T*)v.p + at(v, b, h, t) + 8 * l, u);
-      }
-    }
+    };
+    rows(q, gq, dq, a.wq, dw[0], min(lo, H), min(hi, H));
+    rows(k, gk, dk, a.wk, dw[1], max(lo, H) - H, max(hi, H) - H);
   }
   if (!part) return;
 #pragma unroll
   for (int s = 0; s < 2; ++s)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      float x = dw[s][i];
+      float x = i % 2 ? dw[s][i / 2].y : dw[s][i / 2].x;
 #pragma unroll
       for (int o = LPR; o < 32; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-      if (r0 == 0) sums[warp][s][8 * l + i] = x;
+      if (r0 == 0) sums[warp][s][(i < 4 ? at.lo : at.hi - 4) + i] = x;
     }
   __syncthreads();
   if (threadIdx.x < 2 * D) {
@@ -253,7 +320,7 @@ cudaError_t launch_fwd(la_ctx* ctx, int B, int T_, const la_norm_rope_args& a, c
   const int parts = share(ctx, (int64_t)B * T_, 256 / D);
   const int64_t items = (int64_t)B * T_ * parts, blocks = (items + nr::kWarps - 1) / nr::kWarps;
   ctx->launches += 1;
-  return launch_pdl(nr::norm_rope_kernel<T, D>, dim3((unsigned)(blocks < ctx->sm_count * 8 ? blocks : ctx->sm_count * 8)), dim3(nr::kThreads), 0, s,
+  return launch_pdl(a.interleaved ? nr::norm_rope_kernel<T, D, true> : nr::norm_rope_kernel<T, D, false>, dim3((unsigned)(blocks < ctx->sm_count * 8 ? blocks : ctx->sm_count * 8)), dim3(nr::kThreads), 0, s,
                     pack(a), q, k, qo, ko, ctx->cfg.H, T_, items, parts);
 }
 
@@ -266,7 +333,7 @@ cudaError_t launch_bwd(la_ctx* ctx, int B, int T_, const la_norm_rope_args& a, c
   int64_t blocks = (items + nr::kWarps - 1) / nr::kWarps;
   if (blocks > ctx->sm_count * kBlocksPerSm) blocks = ctx->sm_count * kBlocksPerSm;
   ctx->launches += 1;
-  cudaError_t e = launch_pdl(nr::norm_rope_backward_kernel<T, D>, dim3((unsigned)blocks), dim3(nr::kThreads), 0, s, pack(a), q, k, gq,
+  cudaError_t e = launch_pdl(a.interleaved ? nr::norm_rope_backward_kernel<T, D, true> : nr::norm_rope_backward_kernel<T, D, false>, dim3((unsigned)blocks), dim3(nr::kThreads), 0, s, pack(a), q, k, gq,
                              gk, dq, dk, dwq ? scratch : nullptr, ctx->cfg.H, T_, items, parts);
   if (e != cudaSuccess || !dwq) return e;
   ctx->launches += 1;
