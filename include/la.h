@@ -288,8 +288,15 @@ la_status la_accept_threshold(la_ctx* ctx, int32_t B, int32_t N, const int32_t* 
  *
  * A head whose log_decay is above 0 or NaN, and a sequence whose length is outside 0 .. T, record LA_ERR_INVALID_ARG in
  * the device status and are skipped: their outputs and states are left unwritten, and so is such a sequence's pos.
- * A value of v that is not finite shows in its channel of the tokens from its own on; with the tensor-core kernels
- * also in earlier tokens of its tile of 128.  The same holds for the gradients, in the direction in which they depend. */
+ * A value of v that is not finite shows in its channel of the tokens from its own on; with bf16 io also in earlier tokens
+ * of its block of 32 (counted from the sequence's first token).  The same holds for the gradients, in the direction in
+ * which they depend.
+ *
+ * Kernels: a few tokens are walked one by one in fp32 (both io types).  Longer calls go through the sequence by chunks, bf16
+ * on the tensor cores (tiles of 128 tokens; the scores, the state's copy that the queries read and, in gradients without
+ * dS_in, k in the state's sums are rounded to bf16; S_out and dS_in are fp32 sums whose terms are off by 2^-17 at most),
+ * fp32 on the CUDA cores, every product an fp32 multiply-add.  Few chains of a long sequence are cut over clusters of
+ * thread blocks; there is no workspace.  la_set_prefill_kernel(ctx, 1) walks the tokens of every call. */
 la_status la_decay_prefill(la_ctx* ctx, int32_t B, int32_t T, const la_view* q /*host struct*/, const la_view* k,
                            const la_view* v, const float* log_decay, float scale, const float* S_in, float* S_out,
                            const int32_t* lens, int64_t* pos, const la_view* o, void* stream);

@@ -18,7 +18,7 @@
 // outputs, which are staged where the tile's V was.
 // No factor is formed as lam^i lam^-j, which overflows for heads that forget fast: 32 columns at a time share the exponent
 // of their nearest one, which is never negative, and the diagonal blocks take theirs from a table.
-// Few chains of a long sequence: a cluster of up to 16 blocks takes one chain, a segment each.  Every block first forms
+// Few chains of a long sequence: a cluster of up to 8 blocks takes one chain, a segment each.  Every block first forms
 // the sum of its own segment (K and V are then read twice), leaves it in its shared memory, adds up those before it
 // through distributed shared memory, and all segments run at once.  No workspace, one launch.
 // What bounds it: HBM where chains fill the GPU.  Every wait is bounded; see la_common.cuh.
@@ -38,7 +38,7 @@ constexpr int kRegsA = 48, kRegsB = 80, kRegsC = 72, kRegsIssue = 48;
 static_assert(2 * kRegsA + kRegsB + 4 * kRegsC + kRegsIssue == 8 * 64, "register split");
 constexpr uint32_t BOX = 128 * 128;                // 128 rows x 64 bf16, 128-byte swizzle
 constexpr uint32_t SC_COL = 0, O1_COL = 128, O2_COL = 256, DX_COL = 384, TMEM_COLS = 512;
-constexpr int kMaxSeg = 16;
+constexpr int kMaxSeg = 8;
 
 template <int D, bool LO> struct Map {
   static constexpr uint32_t SLOT = D / 64 * BOX;   // a tile of q, k or v
@@ -143,7 +143,7 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
       : "memory");
 }
 __device__ __forceinline__ uint64_t desc(uint32_t lo);
-// Products of N steps, rolled up but for two steps at a time: the code of all roles shares the instruction cache.
+// Products of several steps, rolled up but for four at a time: the code of all roles shares the instruction cache.
 // Q K^T: both contraction indices run along the 128-byte rows, 4 steps per box of 64.
 template <int N> __device__ __forceinline__ void product_kk(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
 #pragma unroll 1
@@ -830,7 +830,7 @@ static bool make_map(CUtensorMap* m, const la_view& v, int B, int H, int T, int 
 // segments are formed first, so a token costs about 1.5 times as much) pays.
 static int segments(const la_ctx* ctx, int64_t chains, int tiles) {
   int n = 1;
-  while (n < dtc::kMaxSeg / 2 && chains * n * 2 <= ctx->sm_count && tiles >= n * 4) n *= 2;
+  while (n < dtc::kMaxSeg && chains * n * 2 <= ctx->sm_count && tiles >= n * 4) n *= 2;
   return n;
 }
 
