@@ -572,11 +572,6 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
         for (int i = 0; i < NX / 4; ++i)
           *reinterpret_cast<float4*>(smem + M::OFF_LO + (uint32_t)(i * kThreadsC + ct) * 16u) =
               make_float4(X[4 * i], X[4 * i + 1], X[4 * i + 2], X[4 * i + 3]);
-        sync_c();
-        if (ct == 0) {
-          asm volatile("fence.acq_rel.cluster;" ::: "memory");
-          for (int s = rank + 1; s < nseg; ++s) mbar_arrive_remote(bar(B_SHARED), s);
-        }
       }
     }
     // X before the segment: the caller's state, then the sums of the segments before this one
@@ -603,6 +598,15 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
             X[4 * i] = v.x, X[4 * i + 1] = v.y, X[4 * i + 2] = v.z, X[4 * i + 3] = v.w;
           }
         if (LO && nseg == 1) sync_c();             // (the copy and lo go there next)
+      }
+    }
+    // Said only now, with the caller's state read: the last block, which hears it from all the others, may write the state
+    // over it (S_out = S_in), and where its own segment is empty it does so at once.
+    if (LO && nseg > 1 && rank < nseg - 1) {
+      sync_c();
+      if (ct == 0) {
+        asm volatile("fence.acq_rel.cluster;" ::: "memory");
+        for (int s = rank + 1; s < nseg; ++s) mbar_arrive_remote(bar(B_SHARED), s);
       }
     }
     if (LO && nseg > 1) {

@@ -145,6 +145,19 @@ def test_padded_batches(io, d, T, lens, cont):
 
 
 @pytest.mark.parametrize("io,d", TYPES)
+@pytest.mark.parametrize("lens", [None, [130, 1], [700, 0], [2000, 129]])
+def test_state_in_place_over_segments(io, d, lens):
+    """S_out = S_in where a chain is cut into segments, the last ones of them empty: as with a buffer of its own."""
+    c = Case(io, d, 2, 3, 2000, seed=18, cont=True, lens=lens)
+    want = torch.empty_like(c.S_in)
+    o = c.ctx.la_decay_prefill(c.q, c.k, c.v, c.g, c.scale, S_in=c.S_in, S_out=want, lens=c.lens)
+    for _ in range(20):
+        S = c.S_in.clone()
+        got = c.ctx.la_decay_prefill(c.q, c.k, c.v, c.g, c.scale, S_in=S, S_out=S, lens=c.lens)
+        assert torch.equal(got, o) and torch.equal(S, want)
+
+
+@pytest.mark.parametrize("io,d", TYPES)
 @pytest.mark.parametrize("T", [1, 2, 16, 65, 128, 129, 260])
 @pytest.mark.parametrize("cont", [False, True])
 def test_backward_lengths(io, d, T, cont):
