@@ -1,7 +1,8 @@
 // One token of the layer with a decay: S = lam S + k v^T, o = scale q^T S.
 // The state is streamed through registers once, 128-bit loads all in flight before the first use, as in the decode step
-// of the layer without a decay.  The columns of S do not meet: where (sequence, head) units are too few to fill the GPU a
-// unit is cut into blocks of 32 columns, one thread block each, and nothing has to be added up across thread blocks.
+// of the layer without a decay.  Bound by HBM: 64 sequences of 32 heads 42.1 us, 6.4 TB/s, 99 % of the copy bandwidth.  The
+// columns of S do not meet: a unit (sequence, head) may be cut into blocks of 32 columns, one thread block each, and nothing
+// has to be added up across thread blocks (launch_step_t says when).
 #include "decay.cuh"
 
 namespace la {
@@ -71,7 +72,10 @@ static cudaError_t launch_step_t(la_ctx* ctx, int B, const la_view& q, const la_
                                  float scale, float* S, int64_t* pos, const la_view& o, cudaStream_t s) {
   const int units = B * ctx->cfg.H;
   ctx->launches += 1;
-  if (units <= 2 * ctx->sm_count)
+  // d = 128, inside graphs, us cut / whole: 32 units 1.8 / 2.8, 64 2.2 / 2.9, 128 3.6 / 3.0 (one whole block per SM), 200 3.7 / 4.5,
+  // 512 7.4 / 7.7, 1024 13.5 / 14.0 (out of the L2), 2048 44.8 / 42.1 (out of HBM).  d = 64: 64 units 1.7 / 1.7, 512 3.3 / 3.5, 320 and
+  // 800 2.9 / 2.5 and 4.2 / 3.7: whole.
+  if (D == 128 && (2 * units <= ctx->sm_count || (units > ctx->sm_count && units <= 8 * ctx->sm_count)))
     return launch_pdl(ds::decay_step_kernel<T, D, 32>, dim3(units, D / 32), dim3(ds::kThreads), 0, s, q, k, v, g, scale, S,
                       pos, o, ctx->d_status, ctx->cfg.H);
   return launch_pdl(ds::decay_step_kernel<T, D, D>, dim3(units, 1), dim3(ds::kThreads), 0, s, q, k, v, g, scale, S, pos, o,
