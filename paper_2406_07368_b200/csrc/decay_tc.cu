@@ -19,9 +19,12 @@
 // No factor is formed as lam^i lam^-j, which overflows for heads that forget fast: 32 columns at a time share the exponent
 // of their nearest one, which is never negative, and the diagonal blocks take theirs from a table.
 // Few chains of a long sequence: a cluster of up to 8 blocks takes one chain, a segment each.  Every block first forms
-// the sum of its own segment (K and V are then read twice), leaves it in its shared memory, adds up those before it
-// through distributed shared memory, and all segments run at once.  No workspace, one launch.
-// What bounds it: HBM where chains fill the GPU.  Every wait is bounded; see la_common.cuh.
+// the sum of its own segment (K and V are then read twice) and leaves it in its shared memory; through distributed shared
+// memory the blocks turn the sums into the states before the segments, a part of all of them each, and all segments run at
+// once.  No workspace, one launch.
+// What bounds it: shared memory, 5.6 K cycles of 128 bytes per tile (products 2.25 K, warps 2.4 K, TMA 1 K), beside five tile
+// buffers for HBM.  4 x 2048 tokens, 32 heads, d = 128: 63-70 us, 4.0-4.3 TB/s, 0.61-0.66 of the copy bandwidth, tensor pipe 37 %;
+// gradients 147-165 us.  Every wait is bounded; see la_common.cuh.
 #include <cuda.h>
 
 #include "decay.cuh"
@@ -108,6 +111,9 @@ __device__ __forceinline__ float4 ld_cluster(uint32_t addr) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, float4 v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
@@ -302,8 +308,8 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
     mbar_init(bar(B_OD), 1);
     mbar_init(bar(B_OF), kThreadsB);
     mbar_init(bar(B_STAGED), kThreadsB);
-    mbar_init(bar(B_SHARED), rank > 0 ? rank : 1);                 // from every block before this one
-    mbar_init(bar(B_TAKEN), rank < nseg - 1 ? nseg - 1 - rank : 1);  // from every block behind it
+    mbar_init(bar(B_SHARED), nseg);                // from every block of the cluster, this one too
+    mbar_init(bar(B_TAKEN), nseg);
     mbar_init(bar(B_DRAIN), 1);
     ctl.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -574,6 +580,36 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
               make_float4(X[4 * i], X[4 * i + 1], X[4 * i + 2], X[4 * i + 3]);
       }
     }
+    auto tell = [&](int which) {                   // all the cluster's blocks, once all of this block's threads are here
+      sync_c();
+      if (ct == 0) {
+        asm volatile("fence.acq_rel.cluster;" ::: "memory");
+        for (int s = 0; s < nseg; ++s) mbar_arrive_remote(bar(which), s);
+      }
+    };
+    if (LO && nseg > 1) {
+      // The sums of the segments, 64 KB each (d = 128), become the states before the segments, without the caller's, in
+      // place: block r does it for the r-th part of all of them.  Every block then moves as much however many there are.
+      // (With each block reading all the sums before its own a block more cost 4.8 us.)
+      constexpr int NP = NX / 4 * kThreadsC;       // 16-byte pieces of a state
+      tell(B_SHARED);
+      ok = __all_sync(0xffffffffu, mbar_wait_cluster(bar(B_SHARED), 0, abort)) && ok;
+      for (int i = rank * (NP / nseg) + ct; ok && i < (rank + 1) * (NP / nseg); i += kThreadsC) {
+        const uint32_t at = sbase + M::OFF_LO + (uint32_t)i * 16u;
+        float4 sum[kMaxSeg];
+#pragma unroll
+        for (int s = 0; s < kMaxSeg; ++s)
+          if (s < nseg - 1) sum[s] = ld_cluster(map_rank(at, s));
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int s = 0; s < kMaxSeg; ++s)
+          if (s < nseg - 1) {
+            const Fade f = decay_fade(bad ? 0.f : g, s > 0 ? min(max(L, 0), (s + 1) * seg) - min(max(L, 0), s * seg) : 0);
+            x = make_float4(f(x.x) + sum[s].x, f(x.y) + sum[s].y, f(x.z) + sum[s].z, f(x.w) + sum[s].w);
+            st_cluster(map_rank(at, s + 1), x);
+          }
+      }
+    }
     // X before the segment: the caller's state, then the sums of the segments before this one
 #pragma unroll
     for (int i = 0; i < NX; ++i) X[i] = 0.f;
@@ -600,38 +636,22 @@ decay_tc_kernel(const __grid_constant__ Args args, const float* __restrict__ log
         if (LO && nseg == 1) sync_c();             // (the copy and lo go there next)
       }
     }
-    // Said only now, with the caller's state read: the last block, which hears it from all the others, may write the state
-    // over it (S_out = S_in), and where its own segment is empty it does so at once.
-    if (LO && nseg > 1 && rank < nseg - 1) {
-      sync_c();
-      if (ct == 0) {
-        asm volatile("fence.acq_rel.cluster;" ::: "memory");
-        for (int s = rank + 1; s < nseg; ++s) mbar_arrive_remote(bar(B_SHARED), s);
-      }
-    }
     if (LO && nseg > 1) {
+      // (With the caller's state read: the last block, which waits for all the others, may write the state over it.)
+      tell(B_TAKEN);
+      ok = __all_sync(0xffffffffu, mbar_wait_cluster(bar(B_TAKEN), 0, abort)) && ok;
       if (rank > 0) {
-        ok = __all_sync(0xffffffffu, mbar_wait_cluster(bar(B_SHARED), 0, abort)) && ok;
-        for (int s = 0; ok && s < rank; ++s) {
-          const int ls = min(L, (s + 1) * seg) - min(L, s * seg);
-          const Fade f = decay_fade(bad ? 0.f : g, ls > 0 ? ls - (s == 0 ? rev : 0) : 0);
-          const uint32_t from = map_rank(sbase + M::OFF_LO, s);
+        const Fade f = decay_fade(bad ? 0.f : g, n0 > 0 ? n0 - rev : 0);       // (backwards: the gradient as it is)
 #pragma unroll
-          for (int i = 0; i < NX / 4; ++i) {
-            const float4 v = ld_cluster(from + (uint32_t)(i * kThreadsC + ct) * 16u);
-            X[4 * i] = f(X[4 * i]) + v.x;
-            X[4 * i + 1] = f(X[4 * i + 1]) + v.y;
-            X[4 * i + 2] = f(X[4 * i + 2]) + v.z;
-            X[4 * i + 3] = f(X[4 * i + 3]) + v.w;
-            if (i % 4 == 3)                        // (four loads in flight: more would not fit the registers)
-              asm volatile("" : "+f"(X[4 * i - 12]), "+f"(X[4 * i - 8]), "+f"(X[4 * i - 4]), "+f"(X[4 * i]));
-          }
+        for (int i = 0; i < NX / 4; ++i) {
+          const float4 v = *reinterpret_cast<const float4*>(smem + M::OFF_LO + (uint32_t)(i * kThreadsC + ct) * 16u);
+          X[4 * i] = f(X[4 * i]) + v.x;
+          X[4 * i + 1] = f(X[4 * i + 1]) + v.y;
+          X[4 * i + 2] = f(X[4 * i + 2]) + v.z;
+          X[4 * i + 3] = f(X[4 * i + 3]) + v.w;
         }
-        sync_c();
-        if (ct == 0)
-          for (int s = 0; s < rank; ++s) mbar_arrive_remote(bar(B_TAKEN), s);
       }
-      if (rank < nseg - 1) ok = __all_sync(0xffffffffu, mbar_wait_cluster(bar(B_TAKEN), 0, abort)) && ok;
+      sync_c();                                    // the copy and lo go there next
     }
     int left = bad ? 0 : n1 - n0, e = rev && n0 == 0;      // (a sweep backwards starts from the gradient as it is)
     if (ok && left > 0) {
@@ -830,12 +850,43 @@ static bool make_map(CUtensorMap* m, const la_view& v, int B, int H, int T, int 
 
 }  // namespace dtc
 
-// Blocks per chain: one, unless the chains leave SMs idle and a chain is long enough that halving it (the sums of the
-// segments are formed first, so a token costs about 1.5 times as much) pays.
-static int segments(const la_ctx* ctx, int64_t chains, int tiles) {
-  int n = 1;
-  while (n < dtc::kMaxSeg && chains * n * 2 <= ctx->sm_count && tiles >= n * 4) n *= 2;
-  return n;
+// Clusters of n blocks that are resident at once (a block takes an SM; a cluster has to fit one GPC).
+static int resident(la_ctx* ctx, const void* kern, size_t smem, int n) {
+  if (ctx->max_clusters[n] == 0) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(n);
+    cfg.blockDim = dim3(dtc::kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = n;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int got = 0;
+    if (cudaOccupancyMaxActiveClusters(&got, kern, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      got = 0;
+    }
+    ctx->max_clusters[n] = got > 0 ? got : -1;
+  }
+  return ctx->max_clusters[n];
+}
+// Blocks per chain, by what a call costs in units of one tile (2.95 us at d = 128, 2.05 at d = 64), measured inside graphs: whole
+// chains 2 + their tiles; cut into n segments 5 + 1.6 times the longest segment's tiles (K and V are read twice), whatever n; as
+// often as the blocks need to be resident.  (d = 128, us, whole / 2 / 4 / 8: 32 chains of 512 tokens 17.6 / 22.7 / 22.1 / -, 1024
+// 29.6 / 31.5 / 26.6 / 71, 1700 47.3 / 44.5 / 34.5 / 81; 8 chains of 1700 46.7 / 43.7 / 31.2 / 27.2; 16 clusters of 8 are not resident
+// together: 16 chains of 4096 100 / 82 / 50 / 73.)
+static int segments(la_ctx* ctx, const void* kern, size_t smem, int64_t chains, int tiles) {
+  int best = 1;
+  double least = (double)((chains + ctx->sm_count - 1) / ctx->sm_count) * (2.0 + tiles);
+  for (int n = 2; n <= dtc::kMaxSeg && n <= tiles; n *= 2) {
+    const int room = chains * n <= 2 * ctx->sm_count ? resident(ctx, kern, smem, n) : 0;
+    if (room <= 0) continue;
+    const double cost = (double)((chains + room - 1) / room) * (5.0 + 1.6 * ((tiles + n - 1) / n));
+    if (cost < least) least = cost, best = n;
+  }
+  return best;
 }
 
 cudaError_t launch_decay_tc(la_ctx* ctx, int B, int T, const DecayPasses& ps, const float* log_decay, const int32_t* lens,
@@ -863,14 +914,22 @@ cudaError_t launch_decay_tc(la_ctx* ctx, int B, int T, const DecayPasses& ps, co
     if (a.sw[i].mq < 0 || a.sw[i].mk < 0 || a.sw[i].mv < 0 || !dtc::make_map(&a.out[i], p.o, B, c.H, T, c.d)) return cudaErrorInvalidValue;
   }
   const int64_t chains = (int64_t)B * c.H * ps.n;
-  const int nseg = segments(ctx, chains, (T + dtc::TILE - 1) / dtc::TILE);
-  if (chains * nseg > INT32_MAX) return cudaErrorInvalidValue;
-  bool state = nseg > 1 || c.d == 64 || ps.n == 1;   // (a forward call's outputs do not depend on whether it hands out its state)
+  // K~ as one number where no state is handed out and no sums are passed on between segments.  (A forward call's outputs do
+  // not depend on whether it hands out its state.)
+  bool state = c.d == 64 || ps.n == 1;
   for (int i = 0; i < ps.n; ++i) state = state || ps.p[i].S_out;
-  auto kern = c.d == 64 ? dtc::decay_tc_kernel<64, true> : state ? dtc::decay_tc_kernel<128, true> : dtc::decay_tc_kernel<128, false>;
-  const size_t smem = c.d == 64 ? dtc::smem_bytes<64, true>() : state ? dtc::smem_bytes<128, true>() : dtc::smem_bytes<128, false>();
+  auto kern = c.d == 64 ? dtc::decay_tc_kernel<64, true> : dtc::decay_tc_kernel<128, true>;
+  size_t smem = c.d == 64 ? dtc::smem_bytes<64, true>() : dtc::smem_bytes<128, true>();
   cudaError_t e = allow_smem((const void*)kern, ctx->device);
   if (e != cudaSuccess) return e;
+  const int nseg = segments(ctx, (const void*)kern, smem, chains, (T + dtc::TILE - 1) / dtc::TILE);
+  if (chains * nseg > INT32_MAX) return cudaErrorInvalidValue;
+  if (nseg == 1 && !state) {
+    kern = dtc::decay_tc_kernel<128, false>;
+    smem = dtc::smem_bytes<128, false>();
+    e = allow_smem((const void*)kern, ctx->device);
+    if (e != cudaSuccess) return e;
+  }
   ctx->launches += 1;
   const int early = 2 * chains * nseg <= ctx->sm_count;
   return launch_cluster(nseg, early, kern, dim3((unsigned)(chains * nseg)), dim3(dtc::kThreads), smem, s, a, log_decay, lens, pos,
