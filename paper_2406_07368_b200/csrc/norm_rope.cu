@@ -8,6 +8,7 @@
 // the angles of a token, four per lane, are the same for all of them and stay in registers.
 //   turns = p (f / 2 pi) in 64 bits, minus its nearest integer; only that remainder, at most half a turn, goes to fp32
 // (in 32 bits a position of 10^6 alone would leave an angle of the first pair wrong by 0.06).
+// 4 x 2048 tokens, 32 heads, d = 128: 55.6 us, 4.8 TB/s, 75 % of the copy bandwidth; gradients 92.7 us, 67 %.
 // (With eight values in a row per lane whatever the pairs, partners fetched by shuffles and cos, sin and the weights read from
 // shared memory row by row: 4 x 2048 tokens, 32 heads, d = 128: 93 us, gradients 156, 85 % of the L1's throughput.)
 #include "decay.cuh"
@@ -308,7 +309,7 @@ nr::Args pack(const la_norm_rope_args& a) {
   return {a.wq, a.wk, a.inv_freq, a.pos, a.eps, a.mscale, a.norm, a.rot, a.interleaved};
 }
 // A token's rows are shared out until every warp of the GPU has an item, or an item is down to as many rows as a warp
-// takes at a time.
+// takes at a time.  (32 heads, d = 128, us, shared / not: 64 tokens 3.1 / 12.1, 256 6.5 / 12.2, 1024 9.5 / 12.3.)
 int share(const la_ctx* ctx, int64_t tokens, int rows_at_once) {
   const int64_t want = (int64_t)ctx->sm_count * 32;
   int parts = 1;
